@@ -262,6 +262,162 @@ wino_status wino_epilogue_noalloc(const wino_params* p, int32_t vocab, const voi
                                   int32_t* d_cur_tokens, uint8_t* d_mask_bitmap, uint8_t* d_flags,
                                   wino_row_stats* d_stats, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Operators on the caller's own tensors (no context): what a program needs
+ * that keeps keys and values instead of recomputing every row, and the same
+ * for prompts of different lengths.  All are asynchronous on `stream`, which
+ * belongs to the current device, as do the tensors; they allocate nothing,
+ * keep nothing between calls and may be captured into a graph.  Lengths,
+ * positions, slots and page tables are read on the device when the call runs;
+ * sizes the host checks are those passed by value.
+ *
+ * A tensor of rows: element e of head h of row t lies at
+ * data[t * token_stride + h * head_stride + e].  Strides are in elements,
+ * multiples of 8 and not negative; data is 16-byte aligned
+ * (WINO_ERR_UNSUPPORTED otherwise).  Inputs may overlap or repeat (a stride of
+ * 0); the rows and heads of an output must not (strides >= head_dim wherever
+ * there is more than one). */
+typedef struct {
+  void* data;
+  int64_t token_stride, head_stride;
+} wino_heads;
+
+/* A paged cache of keys and values: row `slot` is token slot % page_size of
+ * page slot / page_size; element e of head h of token t of page g lies at
+ * k[g * page_stride + t * token_stride + h * head_stride + e], and at the same
+ * place of v.  page_size is a power of two from 16 to 1024
+ * (WINO_ERR_UNSUPPORTED otherwise).  [page, token, head] and
+ * [page, head, token] orders are both a matter of strides. */
+typedef struct {
+  void *k, *v;
+  int64_t page_stride, token_stride, head_stride;
+  int32_t n_pages, page_size, n_kv_heads, head_dim;
+  int32_t dtype; /* WINO_ACT_BF16 or WINO_ACT_FP16 */
+} wino_kv_cache;
+
+/* Rotary positions.  Pair j < rotary_dim/2 of every head turns by
+ * angle = position * freq[j]:
+ *     y_a = m (x_a cos - x_b sin),  y_b = m (x_b cos + x_a sin)
+ * with (a, b) = (j, j + rotary_dim/2) (WINO_ROPE_HALF, the backbone's layout)
+ * or (2j, 2j + 1) (WINO_ROPE_INTERLEAVED) and m = magnitude; the values from
+ * rotary_dim on are copied.  inverse != 0 turns by -angle: with the same m
+ * that is the transpose, which takes the gradient of the rotated rows to the
+ * gradient of the rows.  rotary_dim is a multiple of 16, at most head_dim;
+ * head_dim is 64 or 128 (WINO_ERR_UNSUPPORTED otherwise).  Angles are taken
+ * in 64 bits and reduced to a fraction of a turn, so far positions lose
+ * nothing; the products are fp32 and rounded once to dtype. */
+#define WINO_ROPE_HALF 0
+#define WINO_ROPE_INTERLEAVED 1
+typedef struct {
+  int32_t head_dim, rotary_dim, layout;
+  int32_t dtype; /* WINO_ACT_BF16 or WINO_ACT_FP16 */
+  int32_t inverse;
+  float magnitude;
+} wino_rope_params;
+
+/* Frequencies for a context longer than the trained one (host arithmetic in
+ * 64 bits; h_freq [rotary_dim/2] in radians per position, and the magnitude
+ * that goes with them).  With f_j = theta^(-2j/rotary_dim):
+ *   WINO_ROPE_SCALE_NONE    f_j
+ *   WINO_ROPE_SCALE_LINEAR  f_j / factor (positions interpolated)
+ *   WINO_ROPE_SCALE_BASE    theta times factor^(r/(r-2)), r = rotary_dim > 2:
+ *                           the slowest pair is slowed by factor, the fastest
+ *                           not at all
+ *   WINO_ROPE_SCALE_PARTS   by parts (arXiv 2309.00071): pairs that turn at
+ *                           least turns_fast times over orig_len positions
+ *                           keep f_j, those below turns_slow times take
+ *                           f_j / factor, between them linear in the number
+ *                           of turns; magnitude 0.1 ln(factor) + 1
+ * WINO_ERR_INVALID_ARG: theta <= 1 or not finite, factor < 1 or not finite,
+ * and for PARTS orig_len <= 0 or turns_fast <= turns_slow. */
+#define WINO_ROPE_SCALE_NONE 0
+#define WINO_ROPE_SCALE_LINEAR 1
+#define WINO_ROPE_SCALE_BASE 2
+#define WINO_ROPE_SCALE_PARTS 3
+typedef struct {
+  int32_t rotary_dim, scaling;
+  double theta, factor, orig_len, turns_fast, turns_slow;
+} wino_rope_config;
+wino_status wino_rope_frequencies(const wino_rope_config* c, double* h_freq, float* h_magnitude);
+
+/* out = x rotated, for n_tokens rows of n_heads heads; out may be x (same
+ * data and strides), else they must not overlap.  d_freq float64
+ * [rotary_dim/2], d_pos int32 [n_tokens] (any value). */
+wino_status wino_rope(const wino_rope_params* p, int64_t n_tokens, int32_t n_heads,
+                      const double* d_freq, const int32_t* d_pos, const wino_heads* x,
+                      const wino_heads* out, void* stream);
+/* The same for the queries (q -> q_out, n_heads heads; q_out may be q), and
+ * for the keys, which go rotated into the cache with the values beside them:
+ * token t to row d_slot[t] (int64 [n_tokens]).  A token whose slot is outside
+ * [0, n_pages * page_size) - a padding row, -1 - leaves the cache as it is.
+ * If two tokens name one slot, which values it ends with is not determined.
+ * p->inverse must be 0 (WINO_ERR_INVALID_ARG). */
+wino_status wino_rope_append(const wino_rope_params* p, const wino_kv_cache* cache,
+                             int64_t n_tokens, int32_t n_heads, const double* d_freq,
+                             const int32_t* d_pos, const int64_t* d_slot, const wino_heads* q,
+                             const wino_heads* k, const wino_heads* v, const wino_heads* q_out,
+                             void* stream);
+
+/* Attention of packed query rows: sequence b owns rows [cu_q[b], cu_q[b+1]),
+ * n_q of them, and n_kv keys; query head h reads KV head
+ * h / (n_heads / n_kv_heads).  Row i of a sequence sees key j < n_kv
+ *   WINO_MASK_FULL    always
+ *   WINO_MASK_CAUSAL  if j <= n_kv - n_q + i: the rows are the last n_q keys'
+ *   WINO_MASK_SHADOW  as in a WINO step (Sec. 4.2.2): the last block_len rows
+ *                     are shadow rows and the last block_len keys the shadow
+ *                     block's.  Other rows see j < n_kv - block_len; shadow
+ *                     row s sees every key but cur_start[b] + s, where
+ *                     cur_start[b] is Y_cur's first key (int32, any value).
+ * o_i = sum_j softmax_j(scale q_i k_j) v_j over the keys it sees; a row that
+ * sees none is zeros.  d_lse (or NULL) fp32 [total_q, n_heads] receives
+ * ln sum_j exp(scale q_i k_j), -inf for such a row.  Values at keys a row does
+ * not see never reach it, whatever they are (NaN, infinities, memory never
+ * written).  Scores, their exponentials' sum and the output accumulate in
+ * fp32; the exponentials are rounded to dtype where they meet the values.
+ * head_dim is 64 or 128 (WINO_ERR_UNSUPPORTED otherwise); scale is finite and
+ * in [1e-6, 1e6]; total_q * n_heads and total_k * n_kv_heads are below 2^31.
+ * Rows of q, out and d_lse from cu_q[batch] on are neither read nor written. */
+#define WINO_MASK_FULL 0
+#define WINO_MASK_CAUSAL 1
+#define WINO_MASK_SHADOW 2
+typedef struct {
+  int32_t n_heads, n_kv_heads, head_dim;
+  int32_t dtype; /* WINO_ACT_BF16 or WINO_ACT_FP16 */
+  int32_t mask, block_len;
+  float scale;
+} wino_attn_params;
+
+/* Device memory the two calls below need for these sizes (0: none, and NULL
+ * may be passed).  Its contents mean nothing between calls; calls that may
+ * overlap need one each.  max_kv_len bounds every sequence's n_kv: longer
+ * ones are cut to it. */
+size_t wino_attention_workspace_bytes(const wino_attn_params* p, int32_t batch, int32_t total_q,
+                                      int32_t max_kv_len);
+
+/* A chunk of new tokens over a paged cache: key j of sequence b is row
+ * j % page_size of page d_page_table[b * table_stride + j / page_size]
+ * (int32; table_width entries per sequence, of which those below
+ * d_kv_len[b] / page_size, rounded up, are read), j < d_kv_len[b] (int32
+ * [batch]).  Keys of a page whose id is outside [0, n_pages) are not seen.
+ * d_cu_q int32 [batch + 1]; d_cur_start int32 [batch], WINO_MASK_SHADOW only.
+ * max_kv_len <= table_width * page_size (WINO_ERR_SHAPE). */
+wino_status wino_paged_attention(const wino_attn_params* p, const wino_kv_cache* cache,
+                                 int32_t batch, int32_t total_q, int32_t max_kv_len,
+                                 const int32_t* d_cu_q, const int32_t* d_kv_len,
+                                 const int32_t* d_page_table, int64_t table_stride,
+                                 int32_t table_width, const int32_t* d_cur_start,
+                                 const wino_heads* q, const wino_heads* out, float* d_lse,
+                                 void* d_workspace, size_t workspace_bytes, void* stream);
+
+/* Whole prompts packed one after another: the keys and values of sequence b
+ * are rows [cu_k[b], cu_k[b+1]) of k and v (total_k rows). */
+wino_status wino_packed_attention(const wino_attn_params* p, int32_t batch, int32_t total_q,
+                                  int32_t total_k, int32_t max_kv_len, const int32_t* d_cu_q,
+                                  const int32_t* d_cu_k, const int32_t* d_cur_start,
+                                  const wino_heads* q, const wino_heads* k, const wino_heads* v,
+                                  const wino_heads* out, float* d_lse, void* d_workspace,
+                                  size_t workspace_bytes, void* stream);
+
 /* Test entry points (same kernels, unfused outputs).
  * wino_debug_logits: fp32 logits [batch, 2*block_len, vocab] of the current
  *   block rows (0..Lb-1) and shadow rows (Lb..2Lb-1) for the given state.

@@ -12,11 +12,14 @@ from __future__ import annotations
 import ctypes as C
 
 from . import _abi
-from ._abi import (WinoError, make_params, wino_create, wino_debug_forward, wino_debug_logits,
+from ._abi import (MASK_CAUSAL, MASK_FULL, MASK_SHADOW, ROPE_HALF, ROPE_INTERLEAVED, ROPE_SCALE_BASE,
+                   ROPE_SCALE_LINEAR, ROPE_SCALE_NONE, ROPE_SCALE_PARTS, WinoError, make_attn_params,
+                   make_kv_cache, make_params, make_rope_params, wino_attention_workspace_bytes, wino_create, wino_debug_forward, wino_debug_logits,
                    wino_debug_gemm, wino_decode, wino_decode_block, wino_destroy, wino_epilogue,
                    wino_epilogue_noalloc,
                    wino_epilogue_workspace_bytes, wino_kernel_class_name, wino_last_error,
-                   wino_profile, wino_profile_read, wino_row_losses, wino_status_string, wino_step,
+                   wino_packed_attention, wino_paged_attention, wino_profile, wino_profile_read, wino_rope,
+                   wino_rope_append, wino_rope_frequencies, wino_row_losses, wino_status_string, wino_step,
                    wino_workspace_bytes)
 
 ACT_BF16, ACT_FP16 = _abi.ACT_BF16, _abi.ACT_FP16
@@ -25,7 +28,10 @@ __all__ = ["WinoModel", "WinoError", "make_params", "ACT_BF16", "ACT_FP16", "win
            "wino_decode_block", "wino_decode", "wino_epilogue", "wino_epilogue_noalloc", "wino_epilogue_workspace_bytes",
            "wino_debug_logits", "wino_debug_forward", "wino_debug_gemm", "wino_profile", "wino_profile_read",
            "wino_kernel_class_name", "wino_status_string", "wino_last_error",
-           "wino_row_losses", "wino_workspace_bytes"]
+           "wino_row_losses", "wino_workspace_bytes", "make_rope_params", "make_attn_params", "make_kv_cache",
+           "ROPE_HALF", "ROPE_INTERLEAVED", "ROPE_SCALE_NONE", "ROPE_SCALE_LINEAR", "ROPE_SCALE_BASE",
+           "ROPE_SCALE_PARTS", "MASK_FULL", "MASK_CAUSAL", "MASK_SHADOW", "wino_rope_frequencies", "wino_rope",
+           "wino_rope_append", "wino_attention_workspace_bytes", "wino_paged_attention", "wino_packed_attention"]
 
 
 def model_config(cfg, act_precision: int = _abi.ACT_BF16) -> _abi.wino_model_config:

@@ -88,7 +88,36 @@ class wino_row_loss(C.Structure):
 
 ROW_LOSS_BYTES = C.sizeof(wino_row_loss)
 
-_vp, _i32, _u32, _sz = C.c_void_p, C.c_int32, C.c_uint32, C.c_size_t
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+ROPE_SCALE_NONE, ROPE_SCALE_LINEAR, ROPE_SCALE_BASE, ROPE_SCALE_PARTS = 0, 1, 2, 3
+MASK_FULL, MASK_CAUSAL, MASK_SHADOW = 0, 1, 2
+
+
+class wino_heads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class wino_kv_cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("page_stride", C.c_int64), ("token_stride", C.c_int64),
+                ("head_stride", C.c_int64), ("n_pages", C.c_int32), ("page_size", C.c_int32),
+                ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32)]
+
+
+class wino_rope_params(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("rotary_dim", C.c_int32), ("layout", C.c_int32), ("dtype", C.c_int32),
+                ("inverse", C.c_int32), ("magnitude", C.c_float)]
+
+
+class wino_rope_config(C.Structure):
+    _fields_ = [("rotary_dim", C.c_int32), ("scaling", C.c_int32), ("theta", C.c_double), ("factor", C.c_double),
+                ("orig_len", C.c_double), ("turns_fast", C.c_double), ("turns_slow", C.c_double)]
+
+
+class wino_attn_params(C.Structure):
+    _fields_ = [("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32),
+                ("mask", C.c_int32), ("block_len", C.c_int32), ("scale", C.c_float)]
+
+_vp, _i32, _u32, _sz, _i64 = C.c_void_p, C.c_int32, C.c_uint32, C.c_size_t, C.c_int64
 _P = C.POINTER
 _protos = {
     "wino_create": (_i32, [_P(wino_model_config), _P(wino_weights), _i32, _i32, _P(_vp)]),
@@ -101,6 +130,15 @@ _protos = {
     "wino_epilogue": (_i32, [_P(wino_params), _i32, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
     "wino_epilogue_noalloc": (_i32, [_P(wino_params), _i32, _vp, _vp, _vp, _vp, _vp, _vp]),
     "wino_row_losses": (_i32, [_vp, _P(wino_params), _vp, _vp, _vp, _vp]),
+    "wino_rope_frequencies": (_i32, [_P(wino_rope_config), _P(C.c_double), _P(C.c_float)]),
+    "wino_rope": (_i32, [_P(wino_rope_params), _i64, _i32, _vp, _vp, _P(wino_heads), _P(wino_heads), _vp]),
+    "wino_rope_append": (_i32, [_P(wino_rope_params), _P(wino_kv_cache), _i64, _i32, _vp, _vp, _vp] +
+                         [_P(wino_heads)] * 4 + [_vp]),
+    "wino_attention_workspace_bytes": (_sz, [_P(wino_attn_params), _i32, _i32, _i32]),
+    "wino_paged_attention": (_i32, [_P(wino_attn_params), _P(wino_kv_cache), _i32, _i32, _i32, _vp, _vp, _vp, _i64,
+                                    _i32, _vp, _P(wino_heads), _P(wino_heads), _vp, _vp, _sz, _vp]),
+    "wino_packed_attention": (_i32, [_P(wino_attn_params), _i32, _i32, _i32, _i32, _vp, _vp, _vp] +
+                              [_P(wino_heads)] * 4 + [_vp, _vp, _sz, _vp]),
     "wino_debug_logits": (_i32, [_vp, _P(wino_params), _vp, _vp, _vp, _vp]),
     "wino_debug_forward": (_i32, [_vp, _P(wino_params), _vp, _vp, _i32, _vp, _vp]),
     "wino_debug_gemm": (_i32, [_vp, _vp, _i32, _i32, _i32, _vp, _vp]),
@@ -126,8 +164,12 @@ try:
     import torch as _torch
     _Tensor, _i32_t, _u8_t = _torch.Tensor, _torch.int32, _torch.uint8
     _f32_t, _bf16_t = _torch.float32, _torch.bfloat16
+    _i64_t, _f64_t = _torch.int64, _torch.float64
+    _act_t = (_bf16_t, _torch.float16)  # by activation type
+    _current_device = _torch._C._cuda_getDevice
 except ImportError:  # int pointers only
-    _torch = _Tensor = _i32_t = _u8_t = _f32_t = _bf16_t = None
+    _torch = _Tensor = _i32_t = _u8_t = _f32_t = _bf16_t = _i64_t = _f64_t = _current_device = None
+    _act_t = (None, None)
 _raw_stream = getattr(_torch._C, "_cuda_getCurrentRawStream", None) if _torch else None
 
 
@@ -262,6 +304,162 @@ def wino_epilogue_noalloc(p: wino_params, vocab: int, logits, cur_tokens, mask_b
                                      _ptr(mask_bitmap, _u8_t, "mask_bitmap"),
                                      _ptr(flags, _u8_t, "flags"), _ptr(stats, None, "stats"),
                                      _stream(stream)), "wino_epilogue_noalloc")
+
+
+# ------------------------------------------------------------------ operators on the caller's tensors
+def _op_ptr(x, dtype, name, numel=None):
+    """_ptr of a tensor of the current device, with at least `numel` elements."""
+    if not isinstance(x, _Tensor):
+        raise TypeError(f"{name}: expected a torch tensor")
+    p = _ptr(x, dtype, name)
+    if x.get_device() != _current_device():
+        raise ValueError(f"{name}: on device {x.get_device()}, the current device is {_current_device()}")
+    if numel is not None and x.numel() < numel:
+        raise ValueError(f"{name}: {x.numel()} elements, {numel} needed")
+    return p
+
+
+def _heads(x, act, n_heads, head_dim, name, n_tokens=None) -> wino_heads:
+    """Rows of heads [tokens, heads, head_dim] with any token and head strides."""
+    if not isinstance(x, _Tensor):
+        raise TypeError(f"{name}: expected a torch tensor")
+    if x.dtype != _act_t[act]:
+        raise TypeError(f"{name}: dtype {x.dtype}, expected {_act_t[act]}")
+    if not x.is_cuda:
+        raise ValueError(f"{name}: must be a device tensor")
+    if x.get_device() != _current_device():
+        raise ValueError(f"{name}: on device {x.get_device()}, the current device is {_current_device()}")
+    sh = x.shape
+    if len(sh) != 3 or sh[1] != n_heads or sh[2] != head_dim or (n_tokens is not None and sh[0] != n_tokens):
+        raise ValueError(f"{name}: shape {tuple(sh)}, expected [{'tokens' if n_tokens is None else n_tokens}, "
+                         f"{n_heads}, {head_dim}]")
+    st = x.stride()
+    if st[2] != 1:
+        raise ValueError(f"{name}: the last axis must be contiguous")
+    # the stride of an axis of length one says nothing, and an empty tensor has no address
+    return wino_heads(x.data_ptr() or 16, st[0] if sh[0] > 1 else n_heads * head_dim,
+                      st[1] if sh[1] > 1 else head_dim)
+
+
+def make_rope_params(head_dim, rotary_dim=None, layout=ROPE_HALF, dtype=ACT_BF16, magnitude=1.0,
+                     inverse=False) -> wino_rope_params:
+    return wino_rope_params(head_dim, head_dim if rotary_dim is None else rotary_dim, layout, dtype, int(inverse),
+                            magnitude)
+
+
+def make_attn_params(n_heads, n_kv_heads, head_dim, dtype=ACT_BF16, mask=MASK_FULL, block_len=0,
+                     scale=None) -> wino_attn_params:
+    """scale: of the scores, 1/sqrt(head_dim) by default."""
+    return wino_attn_params(n_heads, n_kv_heads, head_dim, dtype, mask, block_len,
+                            head_dim ** -0.5 if scale is None else scale)
+
+
+def make_kv_cache(k, v) -> wino_kv_cache:
+    """The cache held by k and v, device tensors [pages, page_size, kv_heads, head_dim] of the same strides
+    (a [pages, kv_heads, page_size, head_dim] cache: its transpose(1, 2)), which stay alive with it."""
+    for x, name in ((k, "k"), (v, "v")):
+        if not isinstance(x, _Tensor) or x.dim() != 4:
+            raise TypeError(f"{name}: expected a tensor [pages, page_size, kv_heads, head_dim]")
+        if x.dtype not in _act_t:
+            raise TypeError(f"{name}: dtype {x.dtype}, expected bfloat16 or float16")
+        if not x.is_cuda:
+            raise ValueError(f"{name}: must be a device tensor")
+        if x.stride(3) != 1:
+            raise ValueError(f"{name}: the last axis must be contiguous")
+    if k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.device != v.device:
+        raise ValueError("k and v must have the same shape, strides, type and device")
+    n, page, heads, hd = k.shape
+    sp, st, sh, _ = k.stride()
+    c = wino_kv_cache(k.data_ptr(), v.data_ptr(), sp if n > 1 else page * heads * hd, st, sh if heads > 1 else hd,
+                      n, page, heads, hd, _act_t.index(k.dtype))
+    c.tensors = (k, v)
+    c.device = k.get_device()
+    return c
+
+
+def _check_cache(cache):
+    if not isinstance(cache, wino_kv_cache):
+        raise TypeError("cache: expected the result of make_kv_cache")
+    if cache.device != _current_device():
+        raise ValueError(f"cache: on device {cache.device}, the current device is {_current_device()}")
+    return C.byref(cache)
+
+
+def wino_rope_frequencies(rotary_dim, theta, scaling=ROPE_SCALE_NONE, factor=1.0, orig_len=4096, turns_fast=32.0,
+                          turns_slow=1.0):
+    """(frequencies in radians per position, a list of rotary_dim/2 floats; the magnitude that goes with them)."""
+    out, mag = (C.c_double * max(rotary_dim // 2, 1))(), C.c_float()
+    c = wino_rope_config(rotary_dim, scaling, theta, factor, orig_len, turns_fast, turns_slow)
+    _check(lib.wino_rope_frequencies(C.byref(c), out, C.byref(mag)), "wino_rope_frequencies")
+    return list(out), mag.value
+
+
+def wino_rope(p: wino_rope_params, freq, pos, x, out, stream=None) -> None:
+    """out = x rotated to positions pos (int32 [tokens]); x and out [tokens, heads, head_dim], out may be x;
+    freq float64 [rotary_dim/2] on the device."""
+    n, h = x.shape[0], x.shape[1]
+    xs = _heads(x, p.dtype, h, p.head_dim, "x")
+    os_ = _heads(out, p.dtype, h, p.head_dim, "out", n)
+    _check(lib.wino_rope(C.byref(p), n, h, _op_ptr(freq, _f64_t, "freq", p.rotary_dim // 2),
+                         _op_ptr(pos, _i32_t, "pos", n) or 16, C.byref(xs), C.byref(os_), _stream(stream)),
+           "wino_rope")
+
+
+def wino_rope_append(p: wino_rope_params, cache: wino_kv_cache, freq, pos, slot, q, k, v, q_out, stream=None) -> None:
+    """q_out = q rotated, and k (rotated) and v into the cache at rows slot (int64 [tokens], outside the cache: not
+    written).  q and q_out [tokens, heads, head_dim], k and v [tokens, kv_heads, head_dim]."""
+    n, h = q.shape[0], q.shape[1]
+    a, hd, hk = p.dtype, p.head_dim, cache.n_kv_heads
+    qs, ks = _heads(q, a, h, hd, "q"), _heads(k, a, hk, hd, "k", n)
+    vs, os_ = _heads(v, a, hk, hd, "v", n), _heads(q_out, a, h, hd, "q_out", n)
+    _check(lib.wino_rope_append(C.byref(p), _check_cache(cache), n, h,
+                                _op_ptr(freq, _f64_t, "freq", p.rotary_dim // 2),
+                                _op_ptr(pos, _i32_t, "pos", n) or 16, _op_ptr(slot, _i64_t, "slot", n) or 16,
+                                C.byref(qs), C.byref(ks), C.byref(vs), C.byref(os_), _stream(stream)),
+           "wino_rope_append")
+
+
+def wino_attention_workspace_bytes(p: wino_attn_params, batch: int, total_q: int, max_kv_len: int) -> int:
+    return int(lib.wino_attention_workspace_bytes(C.byref(p), batch, total_q, max_kv_len))
+
+
+def _attn_common(p, batch, n, cu_q, cur_start, lse, workspace):
+    ws = None if workspace is None else _op_ptr(workspace, None, "workspace")
+    return (_op_ptr(cu_q, _i32_t, "cu_q", batch + 1),
+            None if cur_start is None else _op_ptr(cur_start, _i32_t, "cur_start", batch),
+            None if lse is None else _op_ptr(lse, _f32_t, "lse", n * p.n_heads), ws,
+            0 if ws is None else workspace.numel() * workspace.element_size())
+
+
+def wino_paged_attention(p: wino_attn_params, cache: wino_kv_cache, q, out, cu_q, kv_len, page_table, max_kv_len,
+                         cur_start=None, lse=None, workspace=None, stream=None) -> None:
+    """Attention of the rows q [total_q, heads, head_dim] (sequence b: rows cu_q[b]..cu_q[b+1]) over the cache's pages
+    page_table int32 [batch, width], kv_len int32 [batch] keys each, at most max_kv_len.  lse: float32
+    [total_q, heads] or None; workspace: wino_attention_workspace_bytes, None if that is 0."""
+    n, batch = q.shape[0], kv_len.shape[0]
+    if not isinstance(page_table, _Tensor) or page_table.dim() != 2 or page_table.shape[0] != batch:
+        raise ValueError("page_table: expected a tensor [batch, width]")
+    width = page_table.shape[1]
+    qs, os_ = _heads(q, p.dtype, p.n_heads, p.head_dim, "q"), _heads(out, p.dtype, p.n_heads, p.head_dim, "out", n)
+    cu, cs, ls, ws, wb = _attn_common(p, batch, n, cu_q, cur_start, lse, workspace)
+    _check(lib.wino_paged_attention(C.byref(p), _check_cache(cache), batch, n, max_kv_len, cu,
+                                    _op_ptr(kv_len, _i32_t, "kv_len", batch),
+                                    _op_ptr(page_table, _i32_t, "page_table") or 16, width, width, cs, C.byref(qs),
+                                    C.byref(os_), ls, ws, wb, _stream(stream)), "wino_paged_attention")
+
+
+def wino_packed_attention(p: wino_attn_params, q, k, v, out, cu_q, cu_k, max_kv_len, cur_start=None, lse=None,
+                          workspace=None, stream=None) -> None:
+    """Attention of the rows q [total_q, heads, head_dim] over keys and values [total_k, kv_heads, head_dim], sequence b
+    owning rows cu_q[b]..cu_q[b+1] and keys cu_k[b]..cu_k[b+1] (int32 [batch + 1]), at most max_kv_len keys each.
+    lse and workspace as for wino_paged_attention."""
+    n, nk, batch = q.shape[0], k.shape[0], cu_q.shape[0] - 1
+    qs, os_ = _heads(q, p.dtype, p.n_heads, p.head_dim, "q"), _heads(out, p.dtype, p.n_heads, p.head_dim, "out", n)
+    ks, vs = (_heads(x, p.dtype, p.n_kv_heads, p.head_dim, m, nk) for x, m in ((k, "k"), (v, "v")))
+    cu, cs, ls, ws, wb = _attn_common(p, batch, n, cu_q, cur_start, lse, workspace)
+    _check(lib.wino_packed_attention(C.byref(p), batch, n, nk, max_kv_len, cu,
+                                     _op_ptr(cu_k, _i32_t, "cu_k", batch + 1), cs, C.byref(qs), C.byref(ks),
+                                     C.byref(vs), C.byref(os_), ls, ws, wb, _stream(stream)), "wino_packed_attention")
 
 
 def wino_debug_logits(ctx, p: wino_params, tokens, block_start, logits, stream=None) -> None:

@@ -20,7 +20,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libwino.so")
-SOURCES = ["k_norm.hip", "k_gemm.hip", "k_attn.hip", "k_decide.hip", "wino.cpp"]
+SOURCES = ["k_norm.hip", "k_gemm.hip", "k_attn.hip", "k_decide.hip", "k_rope.hip", "k_seq_attn.hip", "wino.cpp",
+           "operators.cpp"]
 ARCH = "gfx950"
 
 
