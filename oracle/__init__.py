@@ -17,7 +17,9 @@ Everything is plain numpy in float64, computed straight from the definitions:
                  and shadow blocks (the standalone epilogue workload).
 * ``losses``   - per-row entropy, target log-likelihood and greedy confidence
                  of a WINO+ training state (Sec. 5.2-5.3).
+* ``operators`` - rotary positions and attention of packed rows over the keys of
+                 their sequence (the operators on a caller's own tensors).
 
 Readings of points the paper leaves open are stated where they are used.
 """
-from . import model, wino, epilogue, losses  # noqa: F401
+from . import model, wino, epilogue, losses, operators  # noqa: F401
