@@ -342,7 +342,8 @@ wino_status wino_rope_frequencies(const wino_rope_config* c, double* h_freq, flo
 
 /* out = x rotated, for n_tokens rows of n_heads heads; out may be x (same
  * data and strides), else they must not overlap.  d_freq float64
- * [rotary_dim/2], d_pos int32 [n_tokens] (any value). */
+ * [rotary_dim/2], d_pos int32 [n_tokens] (any value); n_tokens is below
+ * 2^26. */
 wino_status wino_rope(const wino_rope_params* p, int64_t n_tokens, int32_t n_heads,
                       const double* d_freq, const int32_t* d_pos, const wino_heads* x,
                       const wino_heads* out, void* stream);
@@ -375,7 +376,8 @@ wino_status wino_rope_append(const wino_rope_params* p, const wino_kv_cache* cac
  * written).  Scores, their exponentials' sum and the output accumulate in
  * fp32; the exponentials are rounded to dtype where they meet the values.
  * head_dim is 64 or 128 (WINO_ERR_UNSUPPORTED otherwise); scale is finite and
- * in [1e-6, 1e6]; total_q * n_heads and total_k * n_kv_heads are below 2^31.
+ * in [1e-6, 1e6]; total_q * n_heads is at most 2^28, batch * n_kv_heads at
+ * most 2^22 and max_kv_len at most 2^30 (WINO_ERR_SHAPE).
  * Rows of q, out and d_lse from cu_q[batch] on are neither read nor written. */
 #define WINO_MASK_FULL 0
 #define WINO_MASK_CAUSAL 1

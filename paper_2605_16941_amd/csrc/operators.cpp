@@ -10,7 +10,11 @@ using namespace wino;
 
 namespace {
 
-constexpr int64_t kMaxRows = (int64_t)1 << 31;
+// A launch holds fewer than 2^32 threads: 64 per rotary token; 256 per 32 rows
+// of attention, one row tile more per sequence and KV head.
+constexpr int64_t kMaxTokens = (int64_t)1 << 26;
+constexpr int64_t kMaxRows = (int64_t)1 << 28;
+constexpr int64_t kMaxSeqHeads = (int64_t)1 << 22;
 
 bool dtype_ok(int32_t d) { return d == WINO_ACT_BF16 || d == WINO_ACT_FP16; }
 bool head_dim_ok(int32_t hd) { return hd == 64 || hd == 128; }
@@ -60,7 +64,7 @@ wino_status check_rope(const wino_rope_params* p, int64_t n_tokens, int32_t n_he
   if (!head_dim_ok(p->head_dim)) return WINO_ERR_UNSUPPORTED;
   if (p->rotary_dim < 1 || p->rotary_dim > p->head_dim) return WINO_ERR_SHAPE;
   if (p->rotary_dim % 16) return WINO_ERR_UNSUPPORTED;
-  if (n_tokens < 0 || n_tokens >= kMaxRows || n_heads < 1 || n_heads > 65535) return WINO_ERR_SHAPE;
+  if (n_tokens < 0 || n_tokens >= kMaxTokens || n_heads < 1 || n_heads > 65535) return WINO_ERR_SHAPE;
   return WINO_OK;
 }
 
@@ -89,7 +93,8 @@ wino_status check_attn(const wino_attn_params* p) {
 
 wino_status check_sizes(const wino_attn_params* p, int32_t batch, int32_t total_q, int32_t max_kv) {
   if (batch < 1 || batch > 65535 || total_q < 0 || max_kv < 0 || max_kv > (1 << 30)) return WINO_ERR_SHAPE;
-  if ((int64_t)total_q * p->n_heads >= kMaxRows) return WINO_ERR_SHAPE;
+  if ((int64_t)total_q * p->n_heads > kMaxRows || (int64_t)batch * p->n_kv_heads > kMaxSeqHeads)
+    return WINO_ERR_SHAPE;
   return WINO_OK;
 }
 
@@ -230,7 +235,7 @@ wino_status wino_packed_attention(const wino_attn_params* p, int32_t batch, int3
   if (s == WINO_OK) s = check_sizes(p, batch, total_q, max_kv_len);
   if (s != WINO_OK) return s;
   if (!d_cu_k) return WINO_ERR_INVALID_ARG;
-  if (total_k < 0 || (int64_t)total_k * p->n_kv_heads >= kMaxRows) return WINO_ERR_SHAPE;
+  if (total_k < 0) return WINO_ERR_SHAPE;
   s = check_heads(k, total_k, p->n_kv_heads, p->head_dim, false);
   if (s == WINO_OK) s = check_heads(v, total_k, p->n_kv_heads, p->head_dim, false);
   if (s != WINO_OK) return s;

@@ -33,7 +33,7 @@ ROPE = dict(head_dim=64, rotary_dim=64, layout=0, dtype=0, inverse=0, magnitude=
 
 @pytest.mark.parametrize("change,status", [
     (dict(head_dim=96), -6), (dict(rotary_dim=0), -2), (dict(rotary_dim=80), -2), (dict(rotary_dim=24), -6),
-    (dict(layout=2), -1), (dict(dtype=2), -1), (dict(magnitude=math.inf), -1), (dict(n=-1), -2), (dict(n=1 << 31), -2),
+    (dict(layout=2), -1), (dict(dtype=2), -1), (dict(magnitude=math.inf), -1), (dict(n=-1), -2), (dict(n=1 << 26), -2),
     (dict(h=0), -2), (dict(freq=None), -1), (dict(pos=None), -1), (dict(x=None), -1), (dict(x=(None, 512, 64)), -1),
     (dict(x=(PTR + 2, 512, 64)), -6), (dict(x=(PTR, 511, 64)), -6), (dict(x=(PTR, -512, 64)), -6),
     (dict(x=(PTR, 512, 65)), -6), (dict(out=(PTR, 56, 64)), -2), (dict(out=(PTR, 512, 0)), -2)])
@@ -110,7 +110,8 @@ BOTH = [(dict(n_heads=7), -2), (dict(n_heads=0), -2), (dict(n_kv_heads=0), -2), 
         (dict(mask=2, block_len=4), -1), (dict(scale=0.0), -1), (dict(scale=float("nan")), -1), (dict(scale=1e9), -1),
         (dict(batch=0), -2), (dict(total_q=-1), -2), (dict(max_kv=-1), -2), (dict(cu_q=None), -1),
         (dict(q=(PTR + 4, 512, 64)), -6), (dict(q=(PTR, 500, 64)), -6), (dict(out=(PTR, 512, 32)), -2),
-        (dict(out=(None, 512, 64)), -1), (dict(total_q=1 << 30), -2)]
+        (dict(out=(None, 512, 64)), -1), (dict(total_q=1 << 30), -2), (dict(batch=1 << 21), -2),
+        (dict(max_kv=(1 << 30) + 1), -2)]
 
 
 @pytest.mark.parametrize("call", [paged, packed])
@@ -128,7 +129,7 @@ def test_paged_attention_refusals(abi, kw, status):
 
 
 @pytest.mark.parametrize("kw,status", [(dict(cu_k=None), -1), (dict(total_k=-1), -2), (dict(k=(PTR, 512, 60)), -6),
-                                       (dict(k=(PTR, -8, 64)), -6), (dict(total_k=1 << 30), -2)])
+                                       (dict(k=(PTR, -8, 64)), -6)])
 def test_packed_attention_refusals(abi, kw, status):
     assert packed(abi, **kw) == status
 
