@@ -15,6 +15,8 @@ namespace {
 constexpr int64_t kMaxTokens = (int64_t)1 << 26;
 constexpr int64_t kMaxRows = (int64_t)1 << 28;
 constexpr int64_t kMaxSeqHeads = (int64_t)1 << 22;
+// 16 rows of keys or values are within 2^31 bytes of each other
+constexpr int64_t kMaxKvStride = (int64_t)1 << 26;
 
 bool dtype_ok(int32_t d) { return d == WINO_ACT_BF16 || d == WINO_ACT_FP16; }
 bool head_dim_ok(int32_t hd) { return hd == 64 || hd == 128; }
@@ -47,7 +49,7 @@ wino_status check_cache(const wino_kv_cache* c, bool written) {
   if (!head_dim_ok(c->head_dim)) return WINO_ERR_UNSUPPORTED;
   if (c->page_size < 16 || c->page_size > 1024 || (c->page_size & (c->page_size - 1)))
     return WINO_ERR_UNSUPPORTED;
-  if (c->page_stride < 0 || c->page_stride % 8) return WINO_ERR_UNSUPPORTED;
+  if (c->page_stride < 0 || c->page_stride % 8 || c->token_stride >= kMaxKvStride) return WINO_ERR_UNSUPPORTED;
   wino_heads rows{c->k, c->token_stride, c->head_stride};
   wino_status s = check_heads(&rows, c->page_size, c->n_kv_heads, c->head_dim, written);
   if (s != WINO_OK) return s;
@@ -239,6 +241,7 @@ wino_status wino_packed_attention(const wino_attn_params* p, int32_t batch, int3
   s = check_heads(k, total_k, p->n_kv_heads, p->head_dim, false);
   if (s == WINO_OK) s = check_heads(v, total_k, p->n_kv_heads, p->head_dim, false);
   if (s != WINO_OK) return s;
+  if (k->token_stride >= kMaxKvStride || v->token_stride >= kMaxKvStride) return WINO_ERR_UNSUPPORTED;
   AttnCall c = attn_call(p, batch, total_q, max_kv_len);
   s = prepare_attn(p, c, d_cu_q, d_cur_start, q, out, d_lse, d_workspace, workspace_bytes);
   if (s != WINO_OK || total_q == 0) return s;

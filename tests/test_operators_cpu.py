@@ -123,13 +123,15 @@ def test_attention_refusals(abi, call, kw, status):
 @pytest.mark.parametrize("kw,status", [
     (dict(kv_len=None), -1), (dict(table=None), -1), (dict(cache=dict(dtype=1)), -1), (dict(cache=dict(v=None)), -1),
     (dict(cache=dict(n_kv_heads=8)), -2), (dict(cache=dict(page_size=48)), -6), (dict(max_kv=97), -2),
-    (dict(width=-1), -2), (dict(table_stride=5), -2), (dict(cache=dict(token_stride=12)), -6)])
+    (dict(width=-1), -2), (dict(table_stride=5), -2), (dict(cache=dict(token_stride=12)), -6),
+    (dict(cache=dict(token_stride=1 << 26)), -6)])
 def test_paged_attention_refusals(abi, kw, status):
     assert paged(abi, **kw) == status
 
 
 @pytest.mark.parametrize("kw,status", [(dict(cu_k=None), -1), (dict(total_k=-1), -2), (dict(k=(PTR, 512, 60)), -6),
-                                       (dict(k=(PTR, -8, 64)), -6)])
+                                       (dict(k=(PTR, -8, 64)), -6),
+                                       (dict(k=(PTR, 1 << 26, 64)), -6)])
 def test_packed_attention_refusals(abi, kw, status):
     assert packed(abi, **kw) == status
 
