@@ -166,9 +166,9 @@ try:
     _f32_t, _bf16_t = _torch.float32, _torch.bfloat16
     _i64_t, _f64_t = _torch.int64, _torch.float64
     _act_t = (_bf16_t, _torch.float16)  # by activation type
-    _current_device = _torch._C._cuda_getDevice
+    _get_device, _cuda_ready = _torch._C._cuda_getDevice, _torch.cuda.is_initialized
 except ImportError:  # int pointers only
-    _torch = _Tensor = _i32_t = _u8_t = _f32_t = _bf16_t = _i64_t = _f64_t = _current_device = None
+    _torch = _Tensor = _i32_t = _u8_t = _f32_t = _bf16_t = _i64_t = _f64_t = _get_device = _cuda_ready = None
     _act_t = (None, None)
 _raw_stream = getattr(_torch._C, "_cuda_getCurrentRawStream", None) if _torch else None
 
@@ -307,38 +307,46 @@ def wino_epilogue_noalloc(p: wino_params, vocab: int, logits, cur_tokens, mask_b
 
 
 # ------------------------------------------------------------------ operators on the caller's tensors
-def _op_ptr(x, dtype, name, numel=None):
-    """_ptr of a tensor of the current device, with at least `numel` elements."""
+def _current_device():
+    return _get_device() if _cuda_ready() else None  # no device tensor exists before
+
+
+def _wrong_device(x, dev, name):
+    if not x.is_cuda:
+        raise ValueError(f"{name}: must be a device tensor")
+    raise ValueError(f"{name}: on device {x.get_device()}, the current device is {dev}")
+
+
+def _op_ptr(x, dtype, name, dev, numel=None):
+    """Device pointer of a contiguous tensor of device `dev` (the current one), with at least `numel` elements."""
     if not isinstance(x, _Tensor):
         raise TypeError(f"{name}: expected a torch tensor")
-    p = _ptr(x, dtype, name)
-    if x.get_device() != _current_device():
-        raise ValueError(f"{name}: on device {x.get_device()}, the current device is {_current_device()}")
+    if x.get_device() != dev:
+        _wrong_device(x, dev, name)
+    if dtype is not None and x.dtype is not dtype:
+        raise TypeError(f"{name}: dtype {x.dtype}, expected {dtype}")
+    if not x.is_contiguous():
+        raise ValueError(f"{name}: must be contiguous")
     if numel is not None and x.numel() < numel:
         raise ValueError(f"{name}: {x.numel()} elements, {numel} needed")
-    return p
+    return x.data_ptr() or 16  # an empty tensor has no address
 
 
-def _heads(x, act, n_heads, head_dim, name, n_tokens=None) -> wino_heads:
+def _heads(x, act, n_heads, head_dim, name, dev, n_tokens) -> wino_heads:
     """Rows of heads [tokens, heads, head_dim] with any token and head strides."""
     if not isinstance(x, _Tensor):
         raise TypeError(f"{name}: expected a torch tensor")
-    if x.dtype != _act_t[act]:
+    if x.dtype is not _act_t[act]:
         raise TypeError(f"{name}: dtype {x.dtype}, expected {_act_t[act]}")
-    if not x.is_cuda:
-        raise ValueError(f"{name}: must be a device tensor")
-    if x.get_device() != _current_device():
-        raise ValueError(f"{name}: on device {x.get_device()}, the current device is {_current_device()}")
-    sh = x.shape
-    if len(sh) != 3 or sh[1] != n_heads or sh[2] != head_dim or (n_tokens is not None and sh[0] != n_tokens):
-        raise ValueError(f"{name}: shape {tuple(sh)}, expected [{'tokens' if n_tokens is None else n_tokens}, "
-                         f"{n_heads}, {head_dim}]")
-    st = x.stride()
-    if st[2] != 1:
+    if x.get_device() != dev:
+        _wrong_device(x, dev, name)
+    if x.shape != (n_tokens, n_heads, head_dim):
+        raise ValueError(f"{name}: shape {tuple(x.shape)}, expected {(n_tokens, n_heads, head_dim)}")
+    ts, hs, es = x.stride()
+    if es != 1:
         raise ValueError(f"{name}: the last axis must be contiguous")
     # the stride of an axis of length one says nothing, and an empty tensor has no address
-    return wino_heads(x.data_ptr() or 16, st[0] if sh[0] > 1 else n_heads * head_dim,
-                      st[1] if sh[1] > 1 else head_dim)
+    return wino_heads(x.data_ptr() or 16, ts if n_tokens > 1 else n_heads * head_dim, hs if n_heads > 1 else head_dim)
 
 
 def make_rope_params(head_dim, rotary_dim=None, layout=ROPE_HALF, dtype=ACT_BF16, magnitude=1.0,
@@ -377,12 +385,12 @@ def make_kv_cache(k, v) -> wino_kv_cache:
     return c
 
 
-def _check_cache(cache):
+def _check_cache(cache, dev):
     if not isinstance(cache, wino_kv_cache):
         raise TypeError("cache: expected the result of make_kv_cache")
-    if cache.device != _current_device():
-        raise ValueError(f"cache: on device {cache.device}, the current device is {_current_device()}")
-    return C.byref(cache)
+    if cache.device != dev:
+        raise ValueError(f"cache: on device {cache.device}, the current device is {dev}")
+    return cache
 
 
 def wino_rope_frequencies(rotary_dim, theta, scaling=ROPE_SCALE_NONE, factor=1.0, orig_len=4096, turns_fast=32.0,
@@ -397,38 +405,28 @@ def wino_rope_frequencies(rotary_dim, theta, scaling=ROPE_SCALE_NONE, factor=1.0
 def wino_rope(p: wino_rope_params, freq, pos, x, out, stream=None) -> None:
     """out = x rotated to positions pos (int32 [tokens]); x and out [tokens, heads, head_dim], out may be x;
     freq float64 [rotary_dim/2] on the device."""
-    n, h = x.shape[0], x.shape[1]
-    xs = _heads(x, p.dtype, h, p.head_dim, "x")
-    os_ = _heads(out, p.dtype, h, p.head_dim, "out", n)
-    _check(lib.wino_rope(C.byref(p), n, h, _op_ptr(freq, _f64_t, "freq", p.rotary_dim // 2),
-                         _op_ptr(pos, _i32_t, "pos", n) or 16, C.byref(xs), C.byref(os_), _stream(stream)),
-           "wino_rope")
+    dev, a, hd = _current_device(), p.dtype, p.head_dim
+    n, h, _ = x.shape
+    xs, os_ = _heads(x, a, h, hd, "x", dev, n), _heads(out, a, h, hd, "out", dev, n)
+    _check(lib.wino_rope(p, n, h, _op_ptr(freq, _f64_t, "freq", dev, p.rotary_dim // 2),
+                         _op_ptr(pos, _i32_t, "pos", dev, n), xs, os_, _stream(stream)), "wino_rope")
 
 
 def wino_rope_append(p: wino_rope_params, cache: wino_kv_cache, freq, pos, slot, q, k, v, q_out, stream=None) -> None:
     """q_out = q rotated, and k (rotated) and v into the cache at rows slot (int64 [tokens], outside the cache: not
     written).  q and q_out [tokens, heads, head_dim], k and v [tokens, kv_heads, head_dim]."""
-    n, h = q.shape[0], q.shape[1]
-    a, hd, hk = p.dtype, p.head_dim, cache.n_kv_heads
-    qs, ks = _heads(q, a, h, hd, "q"), _heads(k, a, hk, hd, "k", n)
-    vs, os_ = _heads(v, a, hk, hd, "v", n), _heads(q_out, a, h, hd, "q_out", n)
-    _check(lib.wino_rope_append(C.byref(p), _check_cache(cache), n, h,
-                                _op_ptr(freq, _f64_t, "freq", p.rotary_dim // 2),
-                                _op_ptr(pos, _i32_t, "pos", n) or 16, _op_ptr(slot, _i64_t, "slot", n) or 16,
-                                C.byref(qs), C.byref(ks), C.byref(vs), C.byref(os_), _stream(stream)),
-           "wino_rope_append")
+    dev, a, hd = _current_device(), p.dtype, p.head_dim
+    hk = _check_cache(cache, dev).n_kv_heads
+    n, h, _ = q.shape
+    qs, ks = _heads(q, a, h, hd, "q", dev, n), _heads(k, a, hk, hd, "k", dev, n)
+    vs, os_ = _heads(v, a, hk, hd, "v", dev, n), _heads(q_out, a, h, hd, "q_out", dev, n)
+    _check(lib.wino_rope_append(p, cache, n, h, _op_ptr(freq, _f64_t, "freq", dev, p.rotary_dim // 2),
+                                _op_ptr(pos, _i32_t, "pos", dev, n), _op_ptr(slot, _i64_t, "slot", dev, n), qs, ks, vs,
+                                os_, _stream(stream)), "wino_rope_append")
 
 
 def wino_attention_workspace_bytes(p: wino_attn_params, batch: int, total_q: int, max_kv_len: int) -> int:
-    return int(lib.wino_attention_workspace_bytes(C.byref(p), batch, total_q, max_kv_len))
-
-
-def _attn_common(p, batch, n, cu_q, cur_start, lse, workspace):
-    ws = None if workspace is None else _op_ptr(workspace, None, "workspace")
-    return (_op_ptr(cu_q, _i32_t, "cu_q", batch + 1),
-            None if cur_start is None else _op_ptr(cur_start, _i32_t, "cur_start", batch),
-            None if lse is None else _op_ptr(lse, _f32_t, "lse", n * p.n_heads), ws,
-            0 if ws is None else workspace.numel() * workspace.element_size())
+    return int(lib.wino_attention_workspace_bytes(p, batch, total_q, max_kv_len))
 
 
 def wino_paged_attention(p: wino_attn_params, cache: wino_kv_cache, q, out, cu_q, kv_len, page_table, max_kv_len,
@@ -436,16 +434,21 @@ def wino_paged_attention(p: wino_attn_params, cache: wino_kv_cache, q, out, cu_q
     """Attention of the rows q [total_q, heads, head_dim] (sequence b: rows cu_q[b]..cu_q[b+1]) over the cache's pages
     page_table int32 [batch, width], kv_len int32 [batch] keys each, at most max_kv_len.  lse: float32
     [total_q, heads] or None; workspace: wino_attention_workspace_bytes, None if that is 0."""
+    dev, a, h, hd = _current_device(), p.dtype, p.n_heads, p.head_dim
+    _check_cache(cache, dev)
     n, batch = q.shape[0], kv_len.shape[0]
-    if not isinstance(page_table, _Tensor) or page_table.dim() != 2 or page_table.shape[0] != batch:
-        raise ValueError("page_table: expected a tensor [batch, width]")
+    table = _op_ptr(page_table, _i32_t, "page_table", dev)
+    if page_table.dim() != 2 or page_table.shape[0] != batch:
+        raise ValueError(f"page_table: shape {tuple(page_table.shape)}, expected [{batch}, width]")
     width = page_table.shape[1]
-    qs, os_ = _heads(q, p.dtype, p.n_heads, p.head_dim, "q"), _heads(out, p.dtype, p.n_heads, p.head_dim, "out", n)
-    cu, cs, ls, ws, wb = _attn_common(p, batch, n, cu_q, cur_start, lse, workspace)
-    _check(lib.wino_paged_attention(C.byref(p), _check_cache(cache), batch, n, max_kv_len, cu,
-                                    _op_ptr(kv_len, _i32_t, "kv_len", batch),
-                                    _op_ptr(page_table, _i32_t, "page_table") or 16, width, width, cs, C.byref(qs),
-                                    C.byref(os_), ls, ws, wb, _stream(stream)), "wino_paged_attention")
+    qs, os_ = _heads(q, a, h, hd, "q", dev, n), _heads(out, a, h, hd, "out", dev, n)
+    _check(lib.wino_paged_attention(
+        p, cache, batch, n, max_kv_len, _op_ptr(cu_q, _i32_t, "cu_q", dev, batch + 1),
+        _op_ptr(kv_len, _i32_t, "kv_len", dev), table, width, width,
+        None if cur_start is None else _op_ptr(cur_start, _i32_t, "cur_start", dev, batch), qs, os_,
+        None if lse is None else _op_ptr(lse, _f32_t, "lse", dev, n * h),
+        None if workspace is None else _op_ptr(workspace, None, "workspace", dev),
+        0 if workspace is None else workspace.nbytes, _stream(stream)), "wino_paged_attention")
 
 
 def wino_packed_attention(p: wino_attn_params, q, k, v, out, cu_q, cu_k, max_kv_len, cur_start=None, lse=None,
@@ -453,13 +456,17 @@ def wino_packed_attention(p: wino_attn_params, q, k, v, out, cu_q, cu_k, max_kv_
     """Attention of the rows q [total_q, heads, head_dim] over keys and values [total_k, kv_heads, head_dim], sequence b
     owning rows cu_q[b]..cu_q[b+1] and keys cu_k[b]..cu_k[b+1] (int32 [batch + 1]), at most max_kv_len keys each.
     lse and workspace as for wino_paged_attention."""
+    dev, a, h, hk, hd = _current_device(), p.dtype, p.n_heads, p.n_kv_heads, p.head_dim
     n, nk, batch = q.shape[0], k.shape[0], cu_q.shape[0] - 1
-    qs, os_ = _heads(q, p.dtype, p.n_heads, p.head_dim, "q"), _heads(out, p.dtype, p.n_heads, p.head_dim, "out", n)
-    ks, vs = (_heads(x, p.dtype, p.n_kv_heads, p.head_dim, m, nk) for x, m in ((k, "k"), (v, "v")))
-    cu, cs, ls, ws, wb = _attn_common(p, batch, n, cu_q, cur_start, lse, workspace)
-    _check(lib.wino_packed_attention(C.byref(p), batch, n, nk, max_kv_len, cu,
-                                     _op_ptr(cu_k, _i32_t, "cu_k", batch + 1), cs, C.byref(qs), C.byref(ks),
-                                     C.byref(vs), C.byref(os_), ls, ws, wb, _stream(stream)), "wino_packed_attention")
+    qs, os_ = _heads(q, a, h, hd, "q", dev, n), _heads(out, a, h, hd, "out", dev, n)
+    ks, vs = _heads(k, a, hk, hd, "k", dev, nk), _heads(v, a, hk, hd, "v", dev, nk)
+    _check(lib.wino_packed_attention(
+        p, batch, n, nk, max_kv_len, _op_ptr(cu_q, _i32_t, "cu_q", dev),
+        _op_ptr(cu_k, _i32_t, "cu_k", dev, batch + 1),
+        None if cur_start is None else _op_ptr(cur_start, _i32_t, "cur_start", dev, batch), qs, ks, vs, os_,
+        None if lse is None else _op_ptr(lse, _f32_t, "lse", dev, n * h),
+        None if workspace is None else _op_ptr(workspace, None, "workspace", dev),
+        0 if workspace is None else workspace.nbytes, _stream(stream)), "wino_packed_attention")
 
 
 def wino_debug_logits(ctx, p: wino_params, tokens, block_start, logits, stream=None) -> None:

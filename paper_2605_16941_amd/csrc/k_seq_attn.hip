@@ -89,49 +89,62 @@ __device__ __forceinline__ Seq seq_of(const AttnCall& c, int b) {
 // workgroups at the end.  (With idle ones between, every other workgroup say,
 // half of the shader engines, which take workgroups in turn, got no work.)
 struct Unit {
-  int b, rem, total;  // sequence, number within it, units in all
+  Seq seq;
+  int b, rem;  // sequence, unit within it (negative: none)
 };
+// Inclusive sum over the lanes: within rows of 16 by DPP row shifts, then the
+// rows' totals by row broadcasts (lane 15 to the next row, lane 31 to the upper
+// half).
 __device__ __forceinline__ int scan_incl(int v) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int x = __shfl_up(v, o, 64);
-    if (lane >= o) v += x;
-  }
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);  // row_shr:1
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);  // row_shr:2
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);  // row_shr:4
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);  // row_shr:8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);  // row_bcast:15 into rows 1, 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);  // row_bcast:31 into rows 2, 3
   return v;
 }
-// count(b): units of sequence b.  find(total) is called once the total is
+// count(s): units of a sequence.  find(total) is called once the total is
 // known and returns the unit to look for, or a negative number for none.
 template <class Count, class Find>
-__device__ __forceinline__ Unit find_unit(int batch, Count count, Find find) {
+__device__ __forceinline__ Unit find_unit(const AttnCall& c, Count count, Find find) {
   const int lane = threadIdx.x & 63;
-  const int strip = (batch + 63) >> 6;  // consecutive sequences per lane
+  const int strip = (c.batch + 63) >> 6;  // consecutive sequences per lane
   int v = 0;
+  Seq mine{};
   for (int j = 0; j < strip; ++j) {
     const int b = lane * strip + j;
-    if (b < batch) v += count(b);
+    if (b < c.batch) {
+      mine = seq_of(c, b);
+      v += count(mine);
+    }
   }
   int incl = scan_incl(v);
   Unit u;
-  u.total = __builtin_amdgcn_readlane(incl, 63);
-  u.rem = find(u.total);
-  u.b = 0;
+  u.rem = find(__builtin_amdgcn_readlane(incl, 63));
   if (u.rem < 0) return u;
-  int at = __popcll(__ballot(incl <= u.rem));  // the lane that holds it
+  int at = min(__popcll(__ballot(incl <= u.rem)), 63);  // the lane that holds it
   if (at) u.rem -= __builtin_amdgcn_readlane(incl, at - 1);
-  u.b = at * strip;
-  if (strip == 1) return u;
-  for (int lo = u.b, end = min(lo + strip, batch); lo < end; lo += 64) {
-    incl = scan_incl(lo + lane < end ? count(lo + lane) : 0);
-    at = __popcll(__ballot(incl <= u.rem));
-    if (at < 64) {
-      if (at) u.rem -= __builtin_amdgcn_readlane(incl, at - 1);
-      u.b = lo + at;
-      return u;
+  u.b = min(at * strip, c.batch - 1);
+  if (strip > 1) {
+    for (int lo = u.b, end = min(lo + strip, c.batch); lo < end; lo += 64) {
+      mine = seq_of(c, min(lo + lane, c.batch - 1));
+      incl = scan_incl(lo + lane < end ? count(mine) : 0);
+      at = __popcll(__ballot(incl <= u.rem));
+      u.b = min(lo + min(at, 63), c.batch - 1);
+      if (at < 64) {
+        if (at) u.rem -= __builtin_amdgcn_readlane(incl, at - 1);
+        break;
+      }
+      u.rem -= __builtin_amdgcn_readlane(incl, 63);
     }
-    u.rem -= __builtin_amdgcn_readlane(incl, 63);
+    at = min(at, 63);
   }
-  return u;  // not reached
+  u.seq.q0 = __builtin_amdgcn_readlane(mine.q0, at);
+  u.seq.nq = __builtin_amdgcn_readlane(mine.nq, at);
+  u.seq.k0 = __builtin_amdgcn_readlane(mine.k0, at);
+  u.seq.nkv = __builtin_amdgcn_readlane(mine.nkv, at);
+  return u;
 }
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -180,8 +193,15 @@ __device__ __forceinline__ void copy_lds(uint32_t lds, const char* base, const u
   }
 }
 
+// Waves per SIMD the registers are kept for: 64-wide heads over packed keys fit
+// a third workgroup (8192 causal rows 324 -> 302 us, 24 prompts of up to 700
+// rows 36.6 -> 33.5); with the page addresses that spills (295 -> 307 us).
+constexpr int attn_waves(int hd, int qw, bool paged) {
+  return qw == 1 && hd == 128 ? 1 : (hd == 64 && qw == 4 && !paged ? 3 : 2);
+}
+
 template <int HD, int QW, bool PAGED, class A>
-__global__ __launch_bounds__(kThreads, QW == 1 && HD == 128 ? 1 : 2) void seq_attn_kernel(AttnCall c, AttnPlan pl) {
+__global__ __launch_bounds__(kThreads, attn_waves(HD, QW, PAGED)) void seq_attn_kernel(AttnCall c, AttnPlan pl) {
   constexpr int KW = 4 / QW;
   constexpr int KB2 = KW == 1 ? 2 : 1;  // 32-key blocks per wave and tile
   constexpr int BKV = 32 * KB2 * KW;    // keys per tile: 64, 64, 128
@@ -205,9 +225,8 @@ __global__ __launch_bounds__(kThreads, QW == 1 && HD == 128 ? 1 : 2) void seq_at
   // causal tiles.  Causal tiles run from the last (longest) to the first.
   int head = 0;
   const Unit unit = find_unit(
-      c.batch,
-      [&](int x) {
-        const Seq q = seq_of(c, x);
+      c,
+      [&](const Seq& q) {
         const int tiles = (q.nq * G + 32 * QW - 1) >> RSHIFT;
         return tiles * max((q.nkv + (1 << pl.chunk_shift) - 1) >> pl.chunk_shift, 1);
       },
@@ -222,15 +241,16 @@ __global__ __launch_bounds__(kThreads, QW == 1 && HD == 128 ? 1 : 2) void seq_at
         head = lin / per_head;
         return lin - head * per_head;
       });
-  const int b = min(unit.b, c.batch - 1);
-  const Seq sq = seq_of(c, b);
+  if (unit.rem < 0) return;
+  const int b = unit.b;
+  const Seq sq = unit.seq;
   const int n_rows = sq.nq * G;
   const int tiles = (n_rows + 32 * QW - 1) >> RSHIFT;
   const int split = unit.rem / max(tiles, 1);
   const int row0 = (tiles - 1 - (unit.rem - split * tiles)) << RSHIFT;
   const int kbeg = split << pl.chunk_shift;
   // (offsets that do not ascend count wrongly: nothing outside the tensors)
-  if (unit.rem < 0 || row0 < 0 || row0 >= n_rows || (split && kbeg >= sq.nkv)) return;
+  if (row0 < 0 || row0 >= n_rows || (split && kbeg >= sq.nkv)) return;
 
   const int tid = threadIdx.x, lane = tid & 63, grp = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -268,7 +288,7 @@ __global__ __launch_bounds__(kThreads, QW == 1 && HD == 128 ? 1 : 2) void seq_at
   // this lane's row: its query and what it sees
   int klim = nkv, excl = -1;
   const bool wave_live = row0 + qw * 32 < n_rows;
-  typename A::v8 qf[KS];
+  const uint16_t* qr;
   {
     const int r = min(row0 + qw * 32 + (lane & 31), n_rows - 1);
     const int tok = r / G, hg = r - tok * G;
@@ -277,9 +297,7 @@ __global__ __launch_bounds__(kThreads, QW == 1 && HD == 128 ? 1 : 2) void seq_at
       if (tok < n_plain) klim = nkv - c.block_len;
       else excl = (int)min((int64_t)cur + (tok - n_plain), (int64_t)0x7FFFFFFF);
     }
-    const uint16_t* qr = c.q.p + (int64_t)(sq.q0 + tok) * c.q.ts + (int64_t)(head * G + hg) * c.q.hs;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) qf[ks] = A::frag(*reinterpret_cast<const uint4*>(qr + ks * 16 + grp * 8));
+    qr = c.q.p + (int64_t)(sq.q0 + tok) * c.q.ts + (int64_t)(head * G + hg) * c.q.hs + grp * 8;
   }
 
   // ---- copies.  Every 16-row group has a uniform base address and fixed
@@ -379,6 +397,8 @@ __global__ __launch_bounds__(kThreads, QW == 1 && HD == 128 ? 1 : 2) void seq_at
   };
   // page ids of tiles t, t + 1, t + 2
   int id0 = 0, id1 = 0, id2 = 0;
+
+  typename A::v8 qf[KS];
 
   // Tile t: its scores are in s.  While their exponentials are taken, the
   // scores of tile t + 1 are computed into sn (the matrix cores and the vector
@@ -498,12 +518,29 @@ __global__ __launch_bounds__(kThreads, QW == 1 && HD == 128 ? 1 : 2) void seq_at
       }
     }
     lrun += psum;
+    // (128-wide heads: V reads two products ahead and a raised priority among
+    // the SIMD's waves, 1170 -> 1132 us at 8192 x 8192 x 32 heads; 64-wide
+    // heads lose 2% to it)
+    constexpr int NV = KB2 * 2 * FE, VA = HD == 128 ? 2 : 0;
+    typename A::v8 vf[VA + 1];
+    if (VA) {
+      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-    for (int ks4 = 0; ks4 < KB2 * 2; ++ks4) {
-      const typename A::v8 pf = A::frag(make_uint4(ph[4 * ks4], ph[4 * ks4 + 1], ph[4 * ks4 + 2], ph[4 * ks4 + 3]));
-#pragma unroll
-      for (int fe = 0; fe < FE; ++fe) oacc[fe] = A::mma(vfrag(par, ks4, fe), pf, oacc[fe]);
+      for (int n = 0; n < VA; ++n) vf[n] = vfrag(par, n / FE, n % FE);
+      __builtin_amdgcn_sched_group_barrier(0x100, 2 * VA, 0);
     }
+#pragma unroll
+    for (int n = 0; n < NV; ++n) {
+      const int ks4 = n / FE, fe = n % FE;
+      if (n + VA < NV) {
+        vf[(n + VA) % (VA + 1)] = vfrag(par, (n + VA) / FE, (n + VA) % FE);
+        if (VA) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      }
+      const typename A::v8 pf = A::frag(make_uint4(ph[4 * ks4], ph[4 * ks4 + 1], ph[4 * ks4 + 2], ph[4 * ks4 + 3]));
+      oacc[fe] = A::mma(vf[n % (VA + 1)], pf, oacc[fe]);
+      if (VA) __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    }
+    if (VA) __builtin_amdgcn_s_setprio(0);
   };
 
   if (ntile > 0) {
@@ -512,14 +549,12 @@ __global__ __launch_bounds__(kThreads, QW == 1 && HD == 128 ? 1 : 2) void seq_at
     id1 = load_ids(1);
     id2 = load_ids(2);
     if (PAGED) asm volatile("" : "+v"(id0), "+v"(id1), "+v"(id2));
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qf[ks]));  // as the ids: loaded before the copies start
     issue(0, false, id0);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = A::frag(*reinterpret_cast<const uint4*>(qr + ks * 16));
     issue(0, true, id0);
     if (ntile > 1) issue(1, false, id1);
-    // K(0) is here; V(0), K(1) (or a second wait's worth of nothing) may not be
-    if (ntile > 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * INS) : "memory");
-    else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(INS) : "memory");
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     zero(s0);
     if (wave_live) {
