@@ -37,7 +37,7 @@
 namespace wino {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256;  // of the merge kernel
 
 struct AttnPlan {
   int splits;       // most key chunks a sequence can have
@@ -196,27 +196,29 @@ __device__ __forceinline__ void copy_lds(uint32_t lds, const char* base, const u
 // Waves per SIMD the registers are kept for: 64-wide heads over packed keys fit
 // a third workgroup (8192 causal rows 324 -> 302 us, 24 prompts of up to 700
 // rows 36.6 -> 33.5); with the page addresses that spills (295 -> 307 us).
+constexpr int attn_threads(int qw) { return qw == 1 ? 128 : 256; }
 constexpr int attn_waves(int hd, int qw, bool paged) {
   return qw == 1 && hd == 128 ? 1 : (hd == 64 && qw == 4 && !paged ? 3 : 2);
 }
 
 template <int HD, int QW, bool PAGED, class A>
-__global__ __launch_bounds__(kThreads, attn_waves(HD, QW, PAGED)) void seq_attn_kernel(AttnCall c, AttnPlan pl) {
-  constexpr int KW = 4 / QW;
+__global__ __launch_bounds__(attn_threads(QW), attn_waves(HD, QW, PAGED)) void seq_attn_kernel(AttnCall c, AttnPlan pl) {
+  constexpr int NT = attn_threads(QW), NW = NT / 64;
+  constexpr int KW = NW / QW;
   constexpr int KB2 = KW == 1 ? 2 : 1;  // 32-key blocks per wave and tile
-  constexpr int BKV = 32 * KB2 * KW;    // keys per tile: 64, 64, 128
+  constexpr int BKV = 32 * KB2 * KW;    // keys per tile: 64
   constexpr int RSHIFT = QW == 1 ? 5 : (QW == 2 ? 6 : 7);
   constexpr int FE = HD / 32, KS = HD / 16, KCH = HD / 8;
   constexpr int KROWS = 1024 / (2 * HD);     // rows per 1 KB copy
-  constexpr int RW = BKV / 4;                // rows each wave copies
+  constexpr int RW = BKV / NW;               // rows each wave copies
   constexpr int INS = RW / KROWS;            // copies per wave and operand
   constexpr int NGW = RW / 16, NG = BKV / 16;  // 16-row groups per wave, per tile
   constexpr int GINS = INS / NGW;            // copies per group
   constexpr int KTILE = BKV * HD, STAGE = 2 * KTILE;
   constexpr int OROW = HD + 4;               // floats per row of the waves' merge
-  constexpr int SMEM = KW > 1 && 128 * OROW * 2 > 2 * STAGE ? 128 * OROW * 2 : 2 * STAGE;
+  constexpr int SMEM = KW > 1 && NW * 32 * OROW * 2 > 2 * STAGE ? NW * 32 * OROW * 2 : 2 * STAGE;
   __shared__ __attribute__((aligned(1024))) uint16_t smem[SMEM];
-  __shared__ float2 sml[KW > 1 ? 4 : 1][32];
+  __shared__ float2 sml[KW > 1 ? NW : 1][32];
 
   const int G = c.hq / c.hk;
   // KV heads spread over the XCDs so that the row tiles of a head meet in one
@@ -276,7 +278,7 @@ __global__ __launch_bounds__(kThreads, attn_waves(HD, QW, PAGED)) void seq_attn_
   const int64_t row_base = (int64_t)sq.q0 * c.hq + (int64_t)head * G;  // of (token 0, head 0 of the group)
   const bool split_out = nkv > (1 << pl.chunk_shift);
   if (split && kbeg >= kend) {  // a chunk of the sequence that this tile does not see
-    for (int r = row0 + tid; r < min(row0 + 32 * QW, n_rows); r += kThreads) {
+    for (int r = row0 + tid; r < min(row0 + 32 * QW, n_rows); r += NT) {
       const int64_t g = row_base + (int64_t)(r / G) * c.hq + r % G;
       pl.part_ml[(int64_t)split * c.total_q * c.hq + g] = make_float2(kNegBig, 0.f);
     }
@@ -442,15 +444,24 @@ __global__ __launch_bounds__(kThreads, attn_waves(HD, QW, PAGED)) void seq_attn_
     asm volatile("" : "+v"(kaddr), "+v"(vaddr));
 
     if (edge) {
-      const int key0 = kv0 + kw * KB2 * 32 + 4 * grp;  // key of register i: key0 + 32 kb2 + 8 (i/4) + i%4
+      // register i of block kb2 holds key key0 + 32 kb2 + 8 (i / 4) + i % 4
+      const int key0 = kv0 + kw * KB2 * 32 + 4 * grp;
+      const int lim = klim - key0;
 #pragma unroll
       for (int kb2 = 0; kb2 < KB2; ++kb2)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int key = key0 + kb2 * 32 + 8 * (i >> 2) + (i & 3);
-          const bool seen = key < klim && key != excl && !((bad >> ((kw * KB2 + kb2) * 2 + (i >> 3))) & 1);
-          s[kb2][i] = seen ? s[kb2][i] : kNegBig;
-        }
+        for (int i = 0; i < 16; ++i)
+          s[kb2][i] = kb2 * 32 + 8 * (i >> 2) + (i & 3) < lim ? s[kb2][i] : kNegBig;
+      if (bad || ex1 > ex0) {
+        const int ex = (int)((uint32_t)excl - (uint32_t)key0);  // (a key that is not excluded from this row: below them all)
+#pragma unroll
+        for (int kb2 = 0; kb2 < KB2; ++kb2)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const bool out = kb2 * 32 + 8 * (i >> 2) + (i & 3) == ex || ((bad >> ((kw * KB2 + kb2) * 2 + (i >> 3))) & 1);
+            s[kb2][i] = out ? kNegBig : s[kb2][i];
+          }
+      }
     }
     float tmax = kNegBig;
 #pragma unroll
@@ -627,7 +638,7 @@ __global__ __launch_bounds__(kThreads, attn_waves(HD, QW, PAGED)) void seq_attn_
       if (grp == 0) sml[KW > 1 ? wave : 0][lane & 31] = make_float2(mrun, lrun);
     }
     __syncthreads();
-    constexpr int TPR = kThreads / (32 * QW);  // threads per row
+    constexpr int TPR = NT / (32 * QW);  // threads per row
     constexpr int EPT = HD / TPR;              // values per thread
     const int rl = tid / TPR, e0 = (tid % TPR) * EPT;
     const int r = row0 + rl;
@@ -682,7 +693,7 @@ __global__ __launch_bounds__(kThreads, attn_waves(HD, QW, PAGED)) void seq_attn_
                                : (int64_t)key * c.v_ts;
       const uint16_t v = vbase[at + e];
       if (!nonfinite<A>(v)) continue;
-      for (int r = row0 + tid / HD; r < min(row0 + 32 * QW, n_rows); r += kThreads / HD) {
+      for (int r = row0 + tid / HD; r < min(row0 + 32 * QW, n_rows); r += NT / HD) {
         const int tk = r / G, hh = r - tk * G;
         int lim = nkv, ex = -1;
         if (c.mask == 1) lim = min(nkv, nkv - sq.nq + tk + 1);
@@ -774,11 +785,11 @@ struct UnitTimes {
 };
 UnitTimes unit_times(int hd, int qw) {
   if (hd == 128) {
-    if (qw == 1) return {256, 3.f, 0.0226f, 0.0114f};
+    if (qw == 1) return {512, 4.4f, 0.044f, 0.018f};
     if (qw == 2) return {512, 7.f, 0.055f, 0.0135f};
     return {512, 8.f, 0.0344f, 0.021f};
   }
-  if (qw == 1) return {512, 3.f, 0.025f, 0.0075f};
+  if (qw == 1) return {1024, 8.f, 0.0477f, 0.0125f};
   if (qw == 2) return {512, 6.f, 0.03f, 0.009f};
   return {512, 7.f, 0.021f, 0.013f};
 }
@@ -832,11 +843,11 @@ hipError_t launch_hd(const AttnCall& c, hipStream_t st) {
   }
   const unsigned grid = (unsigned)(x.units * c.hk);
   if (c.paged) {
-    if (x.qw == 1) seq_attn_kernel<HD, 1, true, A><<<grid, kThreads, 0, st>>>(c, pl);
+    if (x.qw == 1) seq_attn_kernel<HD, 1, true, A><<<grid, attn_threads(1), 0, st>>>(c, pl);
     else if (x.qw == 2) seq_attn_kernel<HD, 2, true, A><<<grid, kThreads, 0, st>>>(c, pl);
     else seq_attn_kernel<HD, 4, true, A><<<grid, kThreads, 0, st>>>(c, pl);
   } else {
-    if (x.qw == 1) seq_attn_kernel<HD, 1, false, A><<<grid, kThreads, 0, st>>>(c, pl);
+    if (x.qw == 1) seq_attn_kernel<HD, 1, false, A><<<grid, attn_threads(1), 0, st>>>(c, pl);
     else if (x.qw == 2) seq_attn_kernel<HD, 2, false, A><<<grid, kThreads, 0, st>>>(c, pl);
     else seq_attn_kernel<HD, 4, false, A><<<grid, kThreads, 0, st>>>(c, pl);
   }
