@@ -378,7 +378,8 @@ wino_status wino_rope_append(const wino_rope_params* p, const wino_kv_cache* cac
  * head_dim is 64 or 128 (WINO_ERR_UNSUPPORTED otherwise); scale is finite and
  * in [1e-6, 1e6]; total_q * n_heads is at most 2^28, batch * n_kv_heads at
  * most 2^22 and max_kv_len at most 2^30 (WINO_ERR_SHAPE).
- * Rows of q, out and d_lse from cu_q[batch] on are neither read nor written. */
+ * Rows of q, out and d_lse before cu_q[0] and from cu_q[batch] on are neither
+ * read nor written.  cu_q (and cu_k) ascend.  out must not overlap an input. */
 #define WINO_MASK_FULL 0
 #define WINO_MASK_CAUSAL 1
 #define WINO_MASK_SHADOW 2
@@ -390,9 +391,10 @@ typedef struct {
 } wino_attn_params;
 
 /* Device memory the two calls below need for these sizes (0: none, and NULL
- * may be passed).  Its contents mean nothing between calls; calls that may
- * overlap need one each.  max_kv_len bounds every sequence's n_kv: longer
- * ones are cut to it. */
+ * may be passed; else 16-byte aligned).  Its contents mean nothing between
+ * calls; calls that may overlap need one each.  max_kv_len bounds every
+ * sequence's n_kv: longer ones are cut to it.  The nearer it is to the longest,
+ * the better the work is divided. */
 size_t wino_attention_workspace_bytes(const wino_attn_params* p, int32_t batch, int32_t total_q,
                                       int32_t max_kv_len);
 

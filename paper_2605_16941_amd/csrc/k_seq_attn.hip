@@ -112,12 +112,12 @@ __device__ __forceinline__ Unit find_unit(const AttnCall& c, Count count, Find f
   const int strip = (c.batch + 63) >> 6;  // consecutive sequences per lane
   int v = 0;
   Seq mine{};
+#pragma unroll 4
   for (int j = 0; j < strip; ++j) {
     const int b = lane * strip + j;
-    if (b < c.batch) {
-      mine = seq_of(c, b);
-      v += count(mine);
-    }
+    mine = seq_of(c, min(b, c.batch - 1));
+    const int n = count(mine);
+    v += b < c.batch ? n : 0;
   }
   int incl = scan_incl(v);
   Unit u;
@@ -174,19 +174,21 @@ __device__ __forceinline__ uint32_t nonfinite(uint32_t w) {
 // kernel), because the compiler otherwise waits for every copy in flight
 // before the next transposing read, which it takes for a write to LDS.  The
 // instruction's offset counts for both addresses; off[j] already has
-// 1024 (N - 1 - j) added and base 1024 (N - 1) subtracted.
+// 1024 (N - 1 - j) added and base 1024 (N - 1) subtracted.  s_nop 4: a scalar
+// that the vector unit wrote (readfirstlane) may be read by a memory
+// instruction five wait states later, which the compiler does not see to here.
 template <int N>
 __device__ __forceinline__ void copy_lds(uint32_t lds, const char* base, const uint32_t* off) {
   if (N == 4) {
     asm volatile(
-        "s_mov_b32 m0, %0\n\ts_nop 0\n\t"
+        "s_mov_b32 m0, %0\n\ts_nop 4\n\t"
         "global_load_lds_dwordx4 %1, %5\n\tglobal_load_lds_dwordx4 %2, %5 offset:1024\n\t"
         "global_load_lds_dwordx4 %3, %5 offset:2048\n\tglobal_load_lds_dwordx4 %4, %5 offset:3072" ::"s"(lds),
         "v"(off[0]), "v"(off[1]), "v"(off[N > 2 ? 2 : 0]), "v"(off[N > 2 ? 3 : 0]), "s"(base)
         : "memory");
   } else {
     asm volatile(
-        "s_mov_b32 m0, %0\n\ts_nop 0\n\t"
+        "s_mov_b32 m0, %0\n\ts_nop 4\n\t"
         "global_load_lds_dwordx4 %1, %3\n\tglobal_load_lds_dwordx4 %2, %3 offset:1024" ::"s"(lds),
         "v"(off[0]), "v"(off[1]), "s"(base)
         : "memory");
@@ -776,7 +778,7 @@ __global__ __launch_bounds__(kThreads) void seq_attn_merge_kernel(AttnCall c, At
 // that length and lengths spread evenly up to it.  Times measured on 28
 // problems (1-256 sequences, 1-2048 rows, 544-16000 keys, both head sizes) with
 // every chunk of 2^8..2^13 keys and none: the choice is 2% behind the best of
-// them in the mean and 7% at most.  Measured both ways: one token of one
+// them in the mean and 8% at most.  Measured both ways: one token of one
 // sequence over 8192 keys, 8 KV heads: 101 us whole, 24 us in chunks of 512;
 // 512 rows over 1000-4000 keys of 16 sequences: 249 us whole, 323 in 1024.
 struct UnitTimes {
@@ -794,6 +796,8 @@ UnitTimes unit_times(int hd, int qw) {
   return {512, 7.f, 0.021f, 0.013f};
 }
 
+constexpr int kWhole = 30, kLargest = 20;  // log2 of the keys of a whole sequence, of the largest chunk
+
 struct Choice {
   int qw, splits, chunk_shift;
   int64_t units;  // per KV head, at most
@@ -809,22 +813,24 @@ Choice choose(const AttnCall& c) {
   const UnitTimes u = unit_times(c.hd, x.qw);
   auto key_time = [&](float units) { return fmaxf(u.alone, u.full * fminf(1.f, units / u.slots)); };
   const float one = (float)tiles * c.hk, part = (float)c.total_q * c.hq * (c.hd + 2) * 8 / 4e6f;
-  x.chunk_shift = 30;
+  x.chunk_shift = kWhole;
   float best = 0.f;
-  for (int cs = 14; cs >= 8; --cs) {  // 14 stands for none
-    const int64_t chunk = cs == 14 ? (int64_t)1 << 30 : (int64_t)1 << cs;
-    if (cs < 14 && chunk >= c.max_kv) continue;
-    const float n = (float)(chunk < c.max_kv ? chunk : c.max_kv);
-    const float s = chunk < c.max_kv ? (float)((c.max_kv + chunk - 1) / chunk) : 1.f;
+  for (int cs = kLargest + 1; cs >= 8; --cs) {  // the first: not split
+    const bool whole = cs > kLargest;
+    const int64_t chunk = (int64_t)1 << (whole ? kWhole : cs);
+    const int64_t ns = c.max_kv > 0 ? (c.max_kv + chunk - 1) / chunk : 1;
+    // (at most 512 chunks, 2^22 workgroups, 2^25 rows to join)
+    if (!whole && (ns < 2 || ns > 512 || (rows / R + c.batch) * ns * c.hk > 1 << 22 || rows * c.hk > 1 << 25)) continue;
+    const float n = (float)(chunk < c.max_kv ? chunk : c.max_kv), s = (float)ns;
     const float us = one * s, ur = one * (s + 1) / 2;
     const float even = ceilf(us / u.slots) * (u.fix + n * key_time(us));
     const float longest = u.fix + n * key_time(ur);
     const float spread = fmaxf(longest, (ur * u.fix + one * c.max_kv / 2 * u.full) / u.slots + longest / 2);
-    const float join = s == 1 ? 0.f : 8 + part * (s + (s + 1) / 2);
+    const float join = whole ? 0.f : 8 + part * (s + (s + 1) / 2);
     const float t = even + spread + join;
-    if (cs == 14 || t < 0.97f * best) {
+    if (whole || t < 0.97f * best) {
       best = t;
-      x.chunk_shift = cs == 14 ? 30 : cs;
+      x.chunk_shift = whole ? kWhole : cs;
     }
   }
   x.splits = c.max_kv > 0 ? (int)((c.max_kv + ((int64_t)1 << x.chunk_shift) - 1) >> x.chunk_shift) : 1;

@@ -189,6 +189,34 @@ def test_long(P, hq, hk, hd, act, page):
         pr.check(pr.paged(P, page))
 
 
+@pytest.mark.parametrize("batch", [64, 65, 200, 4200])
+def test_many_sequences(P, batch):
+    """More sequences than a wave has lanes (and more than 64 per lane), empty ones among them, in every position."""
+    rng = np.random.default_rng(batch)
+    seqs = [(int(n), int(m)) for n, m in zip(rng.integers(0, 3, batch), rng.integers(0, 30, batch))]
+    seqs[-1] = (3, 300)
+    pr = Problem(seqs, 2, 1, 64, 0, "causal")
+    pr.check(pr.paged(P, 16, extra=1))
+    pr.check(pr.packed(P))
+
+
+def test_no_keys_at_all(P):
+    pr = Problem([(3, 0), (70, 0)], 4, 2, 128, 1, "full")
+    pr.check(pr.paged(P, 16, max_kv=0))
+    pr.check(pr.packed(P))
+
+
+def test_a_loose_bound_of_the_lengths(P):
+    """max_kv_len far above every length: more chunks than there are, for few rows and for many."""
+    for seqs in ([(1, 700), (1, 3)], [(40, 300), (5, 5)], [(200, 260)]):
+        pr = Problem(seqs, 4, 2, 64, 0, "causal")
+        pr.paged(P, 16)
+        wide = np.full((len(seqs), 1 << 14), -1)
+        wide[:, :pr.table.shape[1]] = pr.table
+        pr.table = wide
+        pr.check(pr.call_paged(P, max_kv=1 << 18))
+
+
 def test_one_key_heavier_than_all(P):
     """A late key far above the others (the running maximum moves by more than any exponent's range) and scores of
     hundreds in both directions."""
