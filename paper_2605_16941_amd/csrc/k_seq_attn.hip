@@ -200,7 +200,15 @@ __device__ __forceinline__ void copy_lds(uint32_t lds, const char* base, const u
 // rows 36.6 -> 33.5); with the page addresses that spills (295 -> 307 us).
 constexpr int attn_threads(int qw) { return qw == 1 ? 128 : 256; }
 constexpr int attn_waves(int hd, int qw, bool paged) {
-  return qw == 1 && hd == 128 ? 1 : (hd == 64 && qw == 4 && !paged ? 3 : 2);
+  return hd == 64 && qw == 4 && !paged ? 3 : 2;
+}
+// Bytes of LDS for the tiles: two stages of K and V, or the waves' outputs if
+// those are larger.  32 rows: sequences of one tile need one stage, and twice
+// as many workgroups then fit a CU (54 sequences of 11 keys, 32 KV heads:
+// 16 us, with two stages 26).
+constexpr int attn_lds(int hd, int qw, int stages) {
+  const int nw = attn_threads(qw) / 64, tiles = stages * 2 * 64 * hd * 2, outputs = qw < 4 ? nw * 32 * (hd + 4) * 4 : 0;
+  return tiles > outputs ? tiles : outputs;
 }
 
 template <int HD, int QW, bool PAGED, class A>
@@ -218,8 +226,8 @@ __global__ __launch_bounds__(attn_threads(QW), attn_waves(HD, QW, PAGED)) void s
   constexpr int GINS = INS / NGW;            // copies per group
   constexpr int KTILE = BKV * HD, STAGE = 2 * KTILE;
   constexpr int OROW = HD + 4;               // floats per row of the waves' merge
-  constexpr int SMEM = KW > 1 && NW * 32 * OROW * 2 > 2 * STAGE ? NW * 32 * OROW * 2 : 2 * STAGE;
-  __shared__ __attribute__((aligned(1024))) uint16_t smem[SMEM];
+  static_assert(BKV == 64, "attn_lds");
+  extern __shared__ __attribute__((aligned(1024))) uint16_t smem[];
   __shared__ float2 sml[KW > 1 ? NW : 1][32];
 
   const int G = c.hq / c.hk;
@@ -848,14 +856,16 @@ hipError_t launch_hd(const AttnCall& c, hipStream_t st) {
     pl.part_ml = reinterpret_cast<float2*>(pl.part_o + x.splits * rows * HD);
   }
   const unsigned grid = (unsigned)(x.units * c.hk);
+  const int lds = attn_lds(HD, x.qw, x.qw == 1 && c.max_kv <= 64 ? 1 : 2);
+  const dim3 block(attn_threads(x.qw));
   if (c.paged) {
-    if (x.qw == 1) seq_attn_kernel<HD, 1, true, A><<<grid, attn_threads(1), 0, st>>>(c, pl);
-    else if (x.qw == 2) seq_attn_kernel<HD, 2, true, A><<<grid, kThreads, 0, st>>>(c, pl);
-    else seq_attn_kernel<HD, 4, true, A><<<grid, kThreads, 0, st>>>(c, pl);
+    if (x.qw == 1) seq_attn_kernel<HD, 1, true, A><<<grid, block, lds, st>>>(c, pl);
+    else if (x.qw == 2) seq_attn_kernel<HD, 2, true, A><<<grid, block, lds, st>>>(c, pl);
+    else seq_attn_kernel<HD, 4, true, A><<<grid, block, lds, st>>>(c, pl);
   } else {
-    if (x.qw == 1) seq_attn_kernel<HD, 1, false, A><<<grid, attn_threads(1), 0, st>>>(c, pl);
-    else if (x.qw == 2) seq_attn_kernel<HD, 2, false, A><<<grid, kThreads, 0, st>>>(c, pl);
-    else seq_attn_kernel<HD, 4, false, A><<<grid, kThreads, 0, st>>>(c, pl);
+    if (x.qw == 1) seq_attn_kernel<HD, 1, false, A><<<grid, block, lds, st>>>(c, pl);
+    else if (x.qw == 2) seq_attn_kernel<HD, 2, false, A><<<grid, block, lds, st>>>(c, pl);
+    else seq_attn_kernel<HD, 4, false, A><<<grid, block, lds, st>>>(c, pl);
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || x.splits == 1) return e;
