@@ -122,6 +122,28 @@ def test_append_writes_its_slots_and_nothing_else(P, act, hd, hq, hk, page, orde
     assert torch.equal(k, kb) and torch.equal(v, vb)
 
 
+def test_append_in_place_of_the_queries(P):
+    """q_out = q, on a stream given by argument, inside a fused product whose keys and values stay as they are."""
+    n, hq, hk, hd = 37, 6, 2, 64
+    rng = np.random.default_rng(4)
+    qkv = rows(rng, n, hq + 2 * hk, hd, 1)
+    dev = qkv.cuda()
+    kc, vc = (torch.zeros(4, 16, hk, hd, dtype=torch.float16, device="cuda") for _ in range(2))
+    freq, _ = P.wino_rope_frequencies(hd, 1e4, P.ROPE_SCALE_BASE, 4.0)
+    pos = torch.arange(n, dtype=torch.int32)
+    st = torch.cuda.Stream()
+    slot = torch.arange(n, device="cuda") + 5
+    fd, pd = torch.tensor(freq, dtype=torch.float64, device="cuda"), pos.cuda()
+    torch.cuda.synchronize()
+    P.wino_rope_append(P.make_rope_params(hd, dtype=1), P.make_kv_cache(kc, vc), fd, pd, slot, dev[:, :hq],
+                       dev[:, hq:hq + hk], dev[:, hq + hk:], dev[:, :hq], stream=st)
+    torch.cuda.synchronize()
+    check(dev[:, :hq], qkv[:, :hq], pos, freq, hd, 1)
+    assert torch.equal(dev[:, hq:].cpu(), qkv[:, hq:])
+    check(kc.flatten(0, 1)[5:5 + n].cpu(), qkv[:, hq:hq + hk], pos, freq, hd, 1)
+    assert torch.equal(vc.flatten(0, 1)[5:5 + n].cpu(), qkv[:, hq + hk:])
+
+
 def test_append_beyond_32_bits(P):
     """A cache of more than 2^32 elements: the last page's rows are where they belong."""
     hk, hd, page = 2, 128, 64

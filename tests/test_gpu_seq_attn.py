@@ -347,6 +347,31 @@ def test_same_bits_again_on_other_streams_and_in_a_graph(P):
         assert torch.equal(out, eager)
 
 
+def test_two_graphs_with_one_workspace(P):
+    """Two captured calls share a workspace; replayed one after the other in both orders they equal the eager calls."""
+    problems = [Problem([(1, 3000), (1, 900)], 8, 2, 64, 1, seed=1), Problem([(2, 2500), (1, 40)], 4, 1, 128, 0, seed=2)]
+    wants = [pr.paged(P, 32)[0].clone() for pr in problems]
+    calls = [pr.last for pr in problems]
+    need = max(0 if ws is None else ws.numel() for _, ws in calls)
+    assert need  # both are split
+    shared = torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda")
+    st, graphs = torch.cuda.Stream(), []
+    for (args, ws), pr in zip(calls, problems):
+        assert ws is not None
+        g = torch.cuda.CUDAGraph()
+        st.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(st), torch.cuda.graph(g, stream=st):
+            P.wino_paged_attention(*args, workspace=shared)
+        graphs.append(g)
+    for order in ((0, 1), (1, 0), (0, 0, 1)):
+        for i in order:
+            calls[i][0][3].fill_(7)
+            graphs[i].replay()
+        torch.cuda.synchronize()
+        for i in set(order):
+            assert torch.equal(calls[i][0][3], wants[i])
+
+
 def test_cache_beyond_32_bits(P):
     """Pages past element 2^32 of the cache."""
     hk, hd, page = 2, 64, 128

@@ -28,6 +28,12 @@ def cache(abi, **kw):
     return abi.wino_kv_cache(*base.values())
 
 
+def test_struct_sizes_match_header_layout(abi):
+    assert C.sizeof(abi.wino_heads) == 24 and C.sizeof(abi.wino_kv_cache) == 64
+    assert C.sizeof(abi.wino_rope_params) == 24 and C.sizeof(abi.wino_rope_config) == 48
+    assert C.sizeof(abi.wino_attn_params) == 28
+
+
 ROPE = dict(head_dim=64, rotary_dim=64, layout=0, dtype=0, inverse=0, magnitude=1.0)
 
 
