@@ -576,6 +576,10 @@ __global__ __launch_bounds__(attn_threads(QW), attn_waves(HD, QW, PAGED)) void s
     issue(0, true, id0);
     if (ntile > 1) issue(1, false, id1);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    // known to be here: else the compiler, which does not see the copies, waits
+    // for the queries again inside the loop, and with that for copies in flight
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qf[ks]));
     __syncthreads();
     zero(s0);
     if (wave_live) {
