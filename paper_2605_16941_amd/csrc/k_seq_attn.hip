@@ -4,11 +4,18 @@
 //
 // Rows.  The G = n_heads / n_kv_heads query heads that share a KV head are
 // rows of one matrix: row r of a sequence and KV head is token r / G, head
-// r % G of the group.  A workgroup of four waves owns 32*QW such rows and a
-// chunk of the keys; KW = 4 / QW waves share 32 rows and split each tile's
-// keys.  Long prompts take QW = 4 (every wave its own rows, K and V read from
-// LDS by all four); single tokens and blocks take QW = 1 or 2, so that the few
-// rows there are do not leave three waves idle while the keys stream in.
+// r % G of the group.  A workgroup owns 32*QW such rows and a chunk of the
+// keys, 64 of them at a time.  Long prompts take QW = 4: four waves, each its
+// own rows, K and V read from LDS by all four.  Blocks take QW = 2 and single
+// tokens QW = 1: KW = 2 waves share 32 rows and split each tile's keys, so that
+// the few rows there are do not leave waves idle while the keys stream in; they
+// join in LDS at the end.
+//
+// What bounds it, measured: few rows by memory (single tokens of 64 sequences
+// over 8192 keys each, 8 KV heads of 128: 374 us, 5.7 TB/s of keys and values),
+// many rows by the matrix cores and the power they take (8192 x 8192, 32 heads of
+// 128: 1004 us, 1095 TFLOP/s), short sequences by the time until a workgroup's
+// first tile (64 rows over 544 keys of 16 sequences, 32 KV heads: 41 us).
 //
 // Each wave computes S^T = K Q^T (32x32x16 MFMA), so a lane holds 16 keys per
 // 32-key block of ONE row and the softmax's running maximum and sum stay in
@@ -41,7 +48,7 @@ constexpr int kThreads = 256;  // of the merge kernel
 
 struct AttnPlan {
   int splits;       // most key chunks a sequence can have
-  int chunk_shift;  // log2 of the keys per chunk, at least 7
+  int chunk_shift;  // log2 of the keys per chunk, at least 8
   float* part_o;   // [splits][total_q * hq][hd] unnormalised
   float2* part_ml; // [splits][total_q * hq] (maximum, sum)
 };
