@@ -166,9 +166,9 @@ try:
     _f32_t, _bf16_t = _torch.float32, _torch.bfloat16
     _i64_t, _f64_t = _torch.int64, _torch.float64
     _act_t = (_bf16_t, _torch.float16)  # by activation type
-    _get_device, _cuda_ready = _torch._C._cuda_getDevice, _torch.cuda.is_initialized
+    _get_device = getattr(_torch._C, "_cuda_getDevice", None)
 except ImportError:  # int pointers only
-    _torch = _Tensor = _i32_t = _u8_t = _f32_t = _bf16_t = _i64_t = _f64_t = _get_device = _cuda_ready = None
+    _torch = _Tensor = _i32_t = _u8_t = _f32_t = _bf16_t = _i64_t = _f64_t = _get_device = None
     _act_t = (None, None)
 _raw_stream = getattr(_torch._C, "_cuda_getCurrentRawStream", None) if _torch else None
 
@@ -308,7 +308,17 @@ def wino_epilogue_noalloc(p: wino_params, vocab: int, logits, cur_tokens, mask_b
 
 # ------------------------------------------------------------------ operators on the caller's tensors
 def _current_device():
-    return _get_device() if _cuda_ready() else None  # no device tensor exists before
+    try:
+        return _get_device()
+    except Exception:  # no device: there is no device tensor either
+        return None
+
+
+def _stream_on(stream, dev):
+    """_stream, with the current device known."""
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(dev)
+    return _stream(stream)
 
 
 def _wrong_device(x, dev, name):
@@ -409,7 +419,7 @@ def wino_rope(p: wino_rope_params, freq, pos, x, out, stream=None) -> None:
     n, h, _ = x.shape
     xs, os_ = _heads(x, a, h, hd, "x", dev, n), _heads(out, a, h, hd, "out", dev, n)
     _check(lib.wino_rope(p, n, h, _op_ptr(freq, _f64_t, "freq", dev, p.rotary_dim // 2),
-                         _op_ptr(pos, _i32_t, "pos", dev, n), xs, os_, _stream(stream)), "wino_rope")
+                         _op_ptr(pos, _i32_t, "pos", dev, n), xs, os_, _stream_on(stream, dev)), "wino_rope")
 
 
 def wino_rope_append(p: wino_rope_params, cache: wino_kv_cache, freq, pos, slot, q, k, v, q_out, stream=None) -> None:
@@ -422,7 +432,7 @@ def wino_rope_append(p: wino_rope_params, cache: wino_kv_cache, freq, pos, slot,
     vs, os_ = _heads(v, a, hk, hd, "v", dev, n), _heads(q_out, a, h, hd, "q_out", dev, n)
     _check(lib.wino_rope_append(p, cache, n, h, _op_ptr(freq, _f64_t, "freq", dev, p.rotary_dim // 2),
                                 _op_ptr(pos, _i32_t, "pos", dev, n), _op_ptr(slot, _i64_t, "slot", dev, n), qs, ks, vs,
-                                os_, _stream(stream)), "wino_rope_append")
+                                os_, _stream_on(stream, dev)), "wino_rope_append")
 
 
 def wino_attention_workspace_bytes(p: wino_attn_params, batch: int, total_q: int, max_kv_len: int) -> int:
@@ -448,7 +458,7 @@ def wino_paged_attention(p: wino_attn_params, cache: wino_kv_cache, q, out, cu_q
         None if cur_start is None else _op_ptr(cur_start, _i32_t, "cur_start", dev, batch), qs, os_,
         None if lse is None else _op_ptr(lse, _f32_t, "lse", dev, n * h),
         None if workspace is None else _op_ptr(workspace, None, "workspace", dev),
-        0 if workspace is None else workspace.nbytes, _stream(stream)), "wino_paged_attention")
+        0 if workspace is None else workspace.nbytes, _stream_on(stream, dev)), "wino_paged_attention")
 
 
 def wino_packed_attention(p: wino_attn_params, q, k, v, out, cu_q, cu_k, max_kv_len, cur_start=None, lse=None,
@@ -466,7 +476,7 @@ def wino_packed_attention(p: wino_attn_params, q, k, v, out, cu_q, cu_k, max_kv_
         None if cur_start is None else _op_ptr(cur_start, _i32_t, "cur_start", dev, batch), qs, ks, vs, os_,
         None if lse is None else _op_ptr(lse, _f32_t, "lse", dev, n * h),
         None if workspace is None else _op_ptr(workspace, None, "workspace", dev),
-        0 if workspace is None else workspace.nbytes, _stream(stream)), "wino_packed_attention")
+        0 if workspace is None else workspace.nbytes, _stream_on(stream, dev)), "wino_packed_attention")
 
 
 def wino_debug_logits(ctx, p: wino_params, tokens, block_start, logits, stream=None) -> None:
