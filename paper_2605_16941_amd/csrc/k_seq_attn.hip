@@ -189,9 +189,10 @@ __device__ __forceinline__ void copy_lds(uint32_t lds, const char* base, const u
   if (N == 4) {
     asm volatile(
         "s_mov_b32 m0, %0\n\ts_nop 4\n\t"
-        "global_load_lds_dwordx4 %1, %5\n\tglobal_load_lds_dwordx4 %2, %5 offset:1024\n\t"
-        "global_load_lds_dwordx4 %3, %5 offset:2048\n\tglobal_load_lds_dwordx4 %4, %5 offset:3072" ::"s"(lds),
-        "v"(off[0]), "v"(off[1]), "v"(off[N > 2 ? 2 : 0]), "v"(off[N > 2 ? 3 : 0]), "s"(base)
+        "global_load_lds_dwordx4 %1, %5\n\tglobal_load_lds_dwordx4 %2, %5 offset:%6\n\t"
+        "global_load_lds_dwordx4 %3, %5 offset:%7\n\tglobal_load_lds_dwordx4 %4, %5 offset:%8" ::"s"(lds),
+        "v"(off[0]), "v"(off[1]), "v"(off[N > 2 ? 2 : 0]), "v"(off[N > 2 ? 3 : 0]), "s"(base), "n"(1024), "n"(2 * 1024),
+        "n"(3 * 1024)
         : "memory");
   } else {
     asm volatile(
