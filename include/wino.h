@@ -373,7 +373,8 @@ wino_status wino_rope_append(const wino_rope_params* p, const wino_kv_cache* cac
  * sees none is zeros.  d_lse (or NULL) fp32 [total_q, n_heads] receives
  * ln sum_j exp(scale q_i k_j), -inf for such a row.  Values at keys a row does
  * not see never reach it, whatever they are (NaN, infinities, memory never
- * written).  Scores, their exponentials' sum and the output accumulate in
+ * written); NaN and infinities at those it sees always do (an infinity whose
+ * weight is zero in fp32 or dtype may arrive as NaN).  Scores, their exponentials' sum and the output accumulate in
  * fp32; the exponentials are rounded to dtype where they meet the values.
  * head_dim is 64 or 128 (WINO_ERR_UNSUPPORTED otherwise); scale is finite and
  * in [1e-6, 1e6]; total_q * n_heads is at most 2^28, batch * n_kv_heads at

@@ -50,7 +50,7 @@ struct AttnPlan {
   int splits;       // most key chunks a sequence can have
   int chunk_shift;  // log2 of the keys per chunk, at least 8
   float* part_o;   // [splits][total_q * hq][hd] unnormalised
-  float2* part_ml; // [splits][total_q * hq] (maximum, sum)
+  float2* part_ml; // [splits][total_q * hq] (maximum, sum; a sum below zero: part_o is not written)
 };
 
 __device__ __forceinline__ int clampi(int v, int lo, int hi) { return min(max(v, lo), hi); }
@@ -293,7 +293,7 @@ __global__ __launch_bounds__(attn_threads(QW), attn_waves(HD, QW, PAGED)) void s
   if (split && kbeg >= kend) {  // a chunk of the sequence that this tile does not see
     for (int r = row0 + tid; r < min(row0 + 32 * QW, n_rows); r += NT) {
       const int64_t g = row_base + (int64_t)(r / G) * c.hq + r % G;
-      pl.part_ml[(int64_t)split * c.total_q * c.hq + g] = make_float2(kNegBig, 0.f);
+      pl.part_ml[(int64_t)split * c.total_q * c.hq + g] = make_float2(kNegBig, -1.f);
     }
     return;
   }
@@ -752,11 +752,13 @@ __global__ __launch_bounds__(kThreads) void seq_attn_merge_kernel(AttnCall c, At
   const float* p = pl.part_o + g * HD + lane * E;
   for (int s0 = 0; s0 < n; s0 += 64) {
     // a lane per chunk for the weights, then every lane its values of each
-    const float2 ml = s0 + lane < n ? pl.part_ml[(s0 + lane) * rows + g] : make_float2(kNegBig, 0.f);
-    // (sums of zero: chunks that the row, or its whole tile, does not see,
-    // whose outputs need not have been written)
-    const float w = ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f((ml.x - M) * scale_log2);
-    const float l = valu_sum(w * ml.y);
+    const float2 ml = s0 + lane < n ? pl.part_ml[(s0 + lane) * rows + g] : make_float2(kNegBig, -1.f);
+    // Only outputs that were not written are left out.  A chunk whose weight is
+    // zero in fp32 still counts: NaN and infinities at keys the row sees are not
+    // finite however small their weight.
+    const uint64_t unwritten = __ballot(ml.y < 0.f);
+    const float w = __builtin_amdgcn_exp2f((ml.x - M) * scale_log2);
+    const float l = valu_sum(ml.y < 0.f ? 0.f : w * ml.y);
     L += l;
     const int m = min(64, n - s0);
 #pragma unroll 4
@@ -766,7 +768,7 @@ __global__ __launch_bounds__(kThreads) void seq_attn_merge_kernel(AttnCall c, At
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         const float v = q[e];
-        o[e] += ws == 0.f ? 0.f : ws * v;
+        o[e] += (unwritten >> s) & 1 ? 0.f : ws * v;
       }
     }
   }

@@ -436,3 +436,24 @@ def test_prompt_then_blocks_then_tokens(P):
             out2 = torch.empty_like(out)
             P.wino_packed_attention(p, q_out, rk, vd, out2, cud, cud, max(lens), lse=lse, workspace=ws)
             pr.check((out2, lse))
+
+
+def split(pr):
+    """Whether the last paged call cut the keys into chunks: partial outputs are in its workspace."""
+    ws = pr.last[1]
+    return ws is not None and bool((ws != 0xFF).any())
+
+
+@pytest.mark.parametrize("act,hd", [(0, 128), (1, 64)])
+@pytest.mark.parametrize("n", [1, 20, 100])
+def test_nan_at_a_key_far_below_the_maximum_in_another_chunk(P, n, act, hd):
+    """A row's output is over all keys it sees: NaN among the values of a key whose weight is far below the smallest
+    fp32 number (scores of 300 and more between them) reaches the row from another chunk than the heavy key's, in tiles
+    of 32, 64 and 128 rows."""
+    pr = Problem([(n, 1100)], 4, 2, hd, act, "causal", seed=n)
+    pr.q[0][..., 0] = 16
+    pr.k[0][30, :, 0] = 256
+    pr.v[0][700, 0, 3], pr.v[0][600, 1, 7] = float("nan"), float("nan")
+    pr.check(pr.paged(P, 16))
+    assert split(pr)
+    pr.check(pr.packed(P))
