@@ -457,3 +457,45 @@ def test_nan_at_a_key_far_below_the_maximum_in_another_chunk(P, n, act, hd):
     pr.check(pr.paged(P, 16))
     assert split(pr)
     pr.check(pr.packed(P))
+
+
+@pytest.mark.parametrize("mask", ["causal", "shadow", "full"])
+@pytest.mark.parametrize("act,hd", [(0, 128), (1, 64)])
+@pytest.mark.parametrize("n", [2, 20, 200])
+def test_unseen_values_stay_out_of_chunks(P, n, act, hd, mask):
+    """Infinities and NaN among the values where a sequence is cut into chunks, in tiles of 32, 64 and 128 rows: at keys
+    that every row sees, that some rows see, in a chunk that whole tiles do not see, and at the last key."""
+    m, block = 1100, {2: 1, 20: 8, 200: 64}[n]
+    pr = Problem([(n, m)], 4, 2, hd, act, mask, block=block if mask == "shadow" else 0, seed=n)
+    pr.cur = [500]
+    inf, nan = float("inf"), float("nan")
+    for j, e in ((300, 1), (m - 2, 3), (m - n // 2, 5), (m - 1 - n // 8, 7), (500 + block // 2, 9), (m - 1, 11)):
+        pr.v[0][j, 0, e], pr.v[0][j, 0, e + 40], pr.v[0][j, 1, e + 1] = inf, nan, -inf
+    pr.check(pr.paged(P, 16))
+    assert split(pr)
+    pr.check(pr.packed(P))
+
+
+@pytest.mark.parametrize("n", [1, 20, 200])
+@pytest.mark.parametrize("page", [16, 64])
+def test_chunks_of_pages_with_bad_ids(P, n, page):
+    """Pages with ids outside the cache, where a sequence is cut into chunks: one, all of a chunk's, all of the table."""
+    pr = Problem([(n, 1100)], 4, 2, 64, 0, "causal", seed=n)
+    pr.paged(P, page)
+    pages = pr.cache_tensors[0].shape[0]
+    for lo, hi, bad in ((900 // page, 900 // page + 1, pages), (256 // page, 512 // page, -1), (0, 1100, (1 << 31) - 1)):
+        pr.table[:, lo:hi] = bad
+        pr.hidden[0][:, lo * page:hi * page] = True
+        pr.check(pr.call_paged(P))
+        assert split(pr)
+
+
+@pytest.mark.parametrize("n", [1, 20, 200])
+def test_one_key_heavier_than_all_in_its_chunk(P, n):
+    """A key far above the others in one chunk, and far below them in another: the join's weights span all exponents."""
+    pr = Problem([(n, 1100)], 4, 2, 64, 1, "causal", seed=n)
+    pr.k[0][700] = (pr.q[0][-1, 0::2] * 40).to(pr.k[0].dtype)
+    pr.k[0][100] = (pr.q[0][-1, 0::2] * -40).to(pr.k[0].dtype)
+    pr.check(pr.paged(P))
+    assert split(pr)
+    pr.check(pr.packed(P))
