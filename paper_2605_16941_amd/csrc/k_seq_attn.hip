@@ -813,7 +813,23 @@ UnitTimes unit_times(int hd, int qw) {
   return {512, 7.f, 0.021f, 0.013f};
 }
 
-constexpr int kWhole = 30, kLargest = 20;  // log2 of the keys of a whole sequence, of the largest chunk
+// log2 of the keys of a whole sequence, of the largest and of the smallest chunk
+constexpr int kWhole = 30, kLargest = 20, kSmallest = 8;
+constexpr int kMostChunks = 512;
+
+// Partial rows (a row and head of a chunk) a call may have.  It grows with every
+// size, so that a workspace for a program's largest sizes serves its smaller
+// calls, though those may be split where the largest are not.  64 per key and
+// 2^21 hold back what the times below would choose in fewer than 1 of 1000
+// problems of up to 512 sequences, 16384 rows and 131072 keys, where by the
+// same times the next best is 8% behind at most.
+int64_t most_partial_rows(const AttnCall& c) {
+  const int64_t chunks = ((int64_t)c.max_kv + (1 << kSmallest) - 1) >> kSmallest;
+  if (chunks < 2) return 0;
+  const int64_t all = (int64_t)c.total_q * c.hq * (chunks < kMostChunks ? chunks : kMostChunks);
+  const int64_t some = c.max_kv < (1 << 15) ? (int64_t)64 * c.max_kv : 1 << 21;
+  return all < some ? all : some;
+}
 
 struct Choice {
   int qw, splits, chunk_shift;
@@ -830,14 +846,17 @@ Choice choose(const AttnCall& c) {
   const UnitTimes u = unit_times(c.hd, x.qw);
   auto key_time = [&](float units) { return fmaxf(u.alone, u.full * fminf(1.f, units / u.slots)); };
   const float one = (float)tiles * c.hk, part = (float)c.total_q * c.hq * (c.hd + 2) * 8 / 4e6f;
+  const int64_t most_partial = most_partial_rows(c);
   x.chunk_shift = kWhole;
   float best = 0.f;
-  for (int cs = kLargest + 1; cs >= 8; --cs) {  // the first: not split
+  for (int cs = kLargest + 1; cs >= kSmallest; --cs) {  // the first: not split
     const bool whole = cs > kLargest;
     const int64_t chunk = (int64_t)1 << (whole ? kWhole : cs);
     const int64_t ns = c.max_kv > 0 ? (c.max_kv + chunk - 1) / chunk : 1;
-    // (at most 512 chunks, 2^22 workgroups, 2^25 rows to join)
-    if (!whole && (ns < 2 || ns > 512 || (rows / R + c.batch) * ns * c.hk > 1 << 22 || rows * c.hk > 1 << 25)) continue;
+    // (at most 2^22 workgroups, 2^25 rows to join)
+    if (!whole && (ns < 2 || ns > kMostChunks || ns * c.total_q * c.hq > most_partial ||
+                   (rows / R + c.batch) * ns * c.hk > 1 << 22 || rows * c.hk > 1 << 25))
+      continue;
     const float n = (float)(chunk < c.max_kv ? chunk : c.max_kv), s = (float)ns;
     const float us = one * s, ur = one * (s + 1) / 2;
     const float even = ceilf(us / u.slots) * (u.fix + n * key_time(us));
@@ -884,10 +903,7 @@ hipError_t launch_hd(const AttnCall& c, hipStream_t st) {
 
 }  // namespace
 
-size_t attention_workspace(const AttnCall& c) {
-  const Choice x = choose(c);
-  return x.splits > 1 ? (size_t)x.splits * c.total_q * c.hq * (c.hd + 2) * 4 : 0;
-}
+size_t attention_workspace(const AttnCall& c) { return (size_t)most_partial_rows(c) * (c.hd + 2) * 4; }
 
 hipError_t launch_seq_attention(const AttnCall& c, hipStream_t st) {
   if (c.f16) return c.hd == 128 ? launch_hd<128, ActF16>(c, st) : launch_hd<64, ActF16>(c, st);

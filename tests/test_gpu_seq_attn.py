@@ -499,3 +499,20 @@ def test_one_key_heavier_than_all_in_its_chunk(P, n):
     pr.check(pr.paged(P))
     assert split(pr)
     pr.check(pr.packed(P))
+
+
+def test_one_workspace_for_the_largest_sizes(P):
+    """Memory for a program's largest sizes, which are not split, serves smaller calls, which are, and nothing behind it
+    is written."""
+    heads, hd, batch, total, keys = (4, 2), 128, 64, 4096, 1500
+    need = P.wino_attention_workspace_bytes(P.make_attn_params(*heads, hd), batch, total, keys)
+    memory = torch.full((need + 4096,), 0xFF, dtype=torch.uint8, device="cuda")
+    ran_split = 0
+    for n, m in ((1, 1500), (1, 1100), (3, 900), (33, 1400), (130, 1200), (9, 300)):
+        pr = Problem([(n, m), (1, 7)], *heads, hd, 0, "causal", seed=n)
+        pr.workspace = lambda P, p, total, max_kv: memory[:need]
+        memory.fill_(0xFF)
+        pr.check(pr.paged(P, 32))
+        ran_split += split(pr)
+        assert (memory[need:] == 0xFF).all()
+    assert ran_split >= 4

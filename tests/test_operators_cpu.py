@@ -233,3 +233,28 @@ def test_oracle_attention_closed_forms():
     s = oo.sees("shadow", 5, 9, block_len=2, cur_start=3)
     assert s[:3].tolist() == [[True] * 7 + [False] * 2] * 3
     assert [int(x) for x in (~s[3:]).nonzero()[1]] == [3, 4] and (~s[3:]).sum() == 2
+
+
+@pytest.mark.parametrize("heads", [(1, 1), (8, 4), (32, 8), (32, 32), (40, 5)])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_workspace_of_the_largest_sizes_serves_smaller_ones(abi, heads, hd):
+    """A workspace is never larger for fewer sequences, rows or keys, so that a program may allocate one for its largest."""
+    p = abi.make_attn_params(*heads, hd)
+    rng = np.random.default_rng(hd + heads[0])
+    sizes = [[int(x) for x in np.exp(rng.uniform(0, np.log((512, 16384, 262144))))] for _ in range(300)]
+    sizes += [[4, 4, 4096], [4, 4, 2048], [64, 64, 1024], [4, 4, 1024], [1, 32, 8192], [1, 33, 8192], [1, 361, 1024],
+              [1, 362, 1024]]
+    need = np.array([abi.wino_attention_workspace_bytes(p, *s) for s in sizes])
+    sizes = np.array(sizes)
+    for s, n in zip(sizes, need):
+        assert n >= need[(sizes <= s).all(1)].max(), s
+
+
+def test_workspace_of_split_keys(abi):
+    """The refusals of a missing, short or misaligned workspace, at sizes that have one."""
+    p, _ = attn_params(abi, {})
+    need = abi.wino_attention_workspace_bytes(p, 1, 1, 1 << 16)
+    assert need > 0
+    kw = dict(batch=1, total_q=1, max_kv=1 << 16, width=1 << 12, table_stride=1 << 12)
+    assert paged(abi, **kw, ws=None) == -1 and paged(abi, **kw, ws_bytes=need - 1) == -2
+    assert paged(abi, **kw, ws=PTR + 8) == -6
