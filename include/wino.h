@@ -342,8 +342,8 @@ wino_status wino_rope_frequencies(const wino_rope_config* c, double* h_freq, flo
 
 /* out = x rotated, for n_tokens rows of n_heads heads; out may be x (same
  * data and strides), else they must not overlap.  d_freq float64
- * [rotary_dim/2], d_pos int32 [n_tokens] (any value); n_tokens is below
- * 2^26. */
+ * [rotary_dim/2], d_pos int32 [n_tokens] (any value); n_tokens is at
+ * most 2^26 - 4. */
 wino_status wino_rope(const wino_rope_params* p, int64_t n_tokens, int32_t n_heads,
                       const double* d_freq, const int32_t* d_pos, const wino_heads* x,
                       const wino_heads* out, void* stream);

@@ -10,9 +10,10 @@ using namespace wino;
 
 namespace {
 
-// A launch holds fewer than 2^32 threads: 64 per rotary token; 256 per 32 rows
-// of attention, one row tile more per sequence and KV head.
-constexpr int64_t kMaxTokens = (int64_t)1 << 26;
+// A launch holds fewer than 2^32 threads: 64 per rotary token, of which four
+// make a workgroup; 256 per 32 rows of attention, one row tile more per
+// sequence and KV head.
+constexpr int64_t kMaxTokens = ((int64_t)1 << 26) - 4;
 constexpr int64_t kMaxRows = (int64_t)1 << 28;
 constexpr int64_t kMaxSeqHeads = (int64_t)1 << 22;
 // 16 rows of keys or values are within 2^31 bytes of each other
@@ -66,7 +67,7 @@ wino_status check_rope(const wino_rope_params* p, int64_t n_tokens, int32_t n_he
   if (!head_dim_ok(p->head_dim)) return WINO_ERR_UNSUPPORTED;
   if (p->rotary_dim < 1 || p->rotary_dim > p->head_dim) return WINO_ERR_SHAPE;
   if (p->rotary_dim % 16) return WINO_ERR_UNSUPPORTED;
-  if (n_tokens < 0 || n_tokens >= kMaxTokens || n_heads < 1 || n_heads > 65535) return WINO_ERR_SHAPE;
+  if (n_tokens < 0 || n_tokens > kMaxTokens || n_heads < 1 || n_heads > 65535) return WINO_ERR_SHAPE;
   return WINO_OK;
 }
 

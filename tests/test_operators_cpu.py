@@ -258,3 +258,12 @@ def test_workspace_of_split_keys(abi):
     kw = dict(batch=1, total_q=1, max_kv=1 << 16, width=1 << 12, table_stride=1 << 12)
     assert paged(abi, **kw, ws=None) == -1 and paged(abi, **kw, ws_bytes=need - 1) == -2
     assert paged(abi, **kw, ws=PTR + 8) == -6
+
+
+@pytest.mark.parametrize("n,status", [((1 << 26) - 3, -2), ((1 << 26) - 1, -2), ((1 << 26) - 4, -6)])
+def test_most_rotary_tokens(abi, n, status):
+    """A launch of 2^32 threads (64 a token, tokens rounded up to four) does not start: it is refused before; one token
+    fewer passes the sizes' check (and is refused here for its stride)."""
+    prm, x = abi.wino_rope_params(*ROPE.values()), heads(abi, PTR, 511, 64)
+    assert abi.lib.wino_rope(C.byref(prm), n, 4, PTR, PTR, C.byref(x), C.byref(x), None) == status
+    assert append(abi, n=n, q=(PTR, 511, 64)) == status
