@@ -329,7 +329,8 @@ typedef struct {
  *                           f_j / factor, between them linear in the number
  *                           of turns; magnitude 0.1 ln(factor) + 1
  * WINO_ERR_INVALID_ARG: theta <= 1 or not finite, factor < 1 or not finite,
- * and for PARTS orig_len <= 0 or turns_fast <= turns_slow. */
+ * and for PARTS orig_len <= 0 or turns_fast <= turns_slow.  rotary_dim is even,
+ * 2 to 65536 (WINO_ERR_SHAPE). */
 #define WINO_ROPE_SCALE_NONE 0
 #define WINO_ROPE_SCALE_LINEAR 1
 #define WINO_ROPE_SCALE_BASE 2
@@ -343,7 +344,8 @@ wino_status wino_rope_frequencies(const wino_rope_config* c, double* h_freq, flo
 /* out = x rotated, for n_tokens rows of n_heads heads; out may be x (same
  * data and strides), else they must not overlap.  d_freq float64
  * [rotary_dim/2], d_pos int32 [n_tokens] (any value); n_tokens is at
- * most 2^26 - 4. */
+ * most 2^26 - 4, n_heads and the cache's n_kv_heads below at most 65535
+ * (WINO_ERR_SHAPE). */
 wino_status wino_rope(const wino_rope_params* p, int64_t n_tokens, int32_t n_heads,
                       const double* d_freq, const int32_t* d_pos, const wino_heads* x,
                       const wino_heads* out, void* stream);
@@ -377,8 +379,9 @@ wino_status wino_rope_append(const wino_rope_params* p, const wino_kv_cache* cac
  * weight is zero in fp32 or dtype may arrive as NaN).  Scores, their exponentials' sum and the output accumulate in
  * fp32; the exponentials are rounded to dtype where they meet the values.
  * head_dim is 64 or 128 (WINO_ERR_UNSUPPORTED otherwise); scale is finite and
- * in [1e-6, 1e6]; total_q * n_heads is at most 2^28, batch * n_kv_heads at
- * most 2^22 and max_kv_len at most 2^30 (WINO_ERR_SHAPE).
+ * in [1e-6, 1e6] (WINO_ERR_INVALID_ARG).  Sizes (WINO_ERR_SHAPE): total_q *
+ * n_heads is at most 2^28, batch * n_kv_heads at most 2^22, batch 1 to 65535,
+ * n_heads at most 65535, block_len 1 to 2^20 and max_kv_len at most 2^30.
  * Rows of q, out and d_lse before cu_q[0] and from cu_q[batch] on are neither
  * read nor written.  cu_q (and cu_k) ascend.  out must not overlap an input. */
 #define WINO_MASK_FULL 0

@@ -267,3 +267,31 @@ def test_most_rotary_tokens(abi, n, status):
     prm, x = abi.wino_rope_params(*ROPE.values()), heads(abi, PTR, 511, 64)
     assert abi.lib.wino_rope(C.byref(prm), n, 4, PTR, PTR, C.byref(x), C.byref(x), None) == status
     assert append(abi, n=n, q=(PTR, 511, 64)) == status
+
+
+@pytest.mark.parametrize("call", [paged, packed])
+def test_documented_limits_of_attention(abi, call):
+    """Each limit is accepted (the calls go on to the missing offsets) and the next value refused."""
+    one = dict(n_heads=1, n_kv_heads=1, cu_q=None, cache=dict(n_kv_heads=1)) if call is paged else \
+        dict(n_heads=1, n_kv_heads=1, cu_q=None)
+    assert call(abi, **one, batch=65535) == -1 and call(abi, **one, batch=65536) == -2
+    many = dict(n_heads=65535, n_kv_heads=1)
+    assert call(abi, **{**one, **many}) == -1 and call(abi, **{**one, **many, "n_heads": 65536}) == -2
+    sh = dict(mask=2, cur=PTR)
+    assert call(abi, **one, **sh, block_len=1 << 20) == -1 and call(abi, **one, **sh, block_len=(1 << 20) + 1) == -2
+    assert call(abi, **one, batch=65535, total_q=1 << 28) == -1
+    assert call(abi, **one, total_q=(1 << 28) + 1) == -2
+
+
+def test_documented_limits_of_rope(abi):
+    x = heads(abi, PTR, 1 << 23, 65)  # a head stride that is refused after the sizes
+    for n_heads, status in ((65535, -6), (65536, -2)):
+        prm = abi.wino_rope_params(*ROPE.values())
+        assert abi.lib.wino_rope(C.byref(prm), 5, n_heads, PTR, PTR, C.byref(x), C.byref(x), None) == status
+    big = dict(token_stride=1 << 23, page_stride=1 << 27)
+    assert append(abi, cache_args=dict(n_kv_heads=65535, **big), k=(PTR, 511, 64)) == -6
+    assert append(abi, cache_args=dict(n_kv_heads=65536, **big), k=(PTR, 511, 64)) == -2
+    assert len(abi.wino_rope_frequencies(65536, 1e4)[0]) == 32768
+    with pytest.raises(abi.WinoError) as e:
+        abi.wino_rope_frequencies(65538, 1e4)
+    assert e.value.status == -2
