@@ -307,6 +307,12 @@ def wino_epilogue_noalloc(p: wino_params, vocab: int, logits, cur_tokens, mask_b
 
 
 # ------------------------------------------------------------------ operators on the caller's tensors
+def _fit(n):
+    """n for a 32-bit argument, of which ctypes would take the lower bits: the nearest number that fits, which every
+    limit refuses (counts of keys and pages, which 32-bit offsets and ids index, have none and need no more)."""
+    return n if -0x80000000 <= n <= 0x7FFFFFFF else (0x7FFFFFFF if n > 0 else -0x80000000)
+
+
 def _current_device():
     try:
         return _get_device()
@@ -361,14 +367,14 @@ def _heads(x, act, n_heads, head_dim, name, dev, n_tokens) -> wino_heads:
 
 def make_rope_params(head_dim, rotary_dim=None, layout=ROPE_HALF, dtype=ACT_BF16, magnitude=1.0,
                      inverse=False) -> wino_rope_params:
-    return wino_rope_params(head_dim, head_dim if rotary_dim is None else rotary_dim, layout, dtype, int(inverse),
-                            magnitude)
+    return wino_rope_params(_fit(head_dim), _fit(head_dim if rotary_dim is None else rotary_dim), _fit(layout),
+                            _fit(dtype), int(bool(inverse)), magnitude)
 
 
 def make_attn_params(n_heads, n_kv_heads, head_dim, dtype=ACT_BF16, mask=MASK_FULL, block_len=0,
                      scale=None) -> wino_attn_params:
     """scale: of the scores, 1/sqrt(head_dim) by default."""
-    return wino_attn_params(n_heads, n_kv_heads, head_dim, dtype, mask, block_len,
+    return wino_attn_params(_fit(n_heads), _fit(n_kv_heads), _fit(head_dim), _fit(dtype), _fit(mask), _fit(block_len),
                             head_dim ** -0.5 if scale is None else scale)
 
 
@@ -389,7 +395,7 @@ def make_kv_cache(k, v) -> wino_kv_cache:
     n, page, heads, hd = k.shape
     sp, st, sh, _ = k.stride()
     c = wino_kv_cache(k.data_ptr(), v.data_ptr(), sp if n > 1 else page * heads * hd, st, sh if heads > 1 else hd,
-                      n, page, heads, hd, _act_t.index(k.dtype))
+                      _fit(n), _fit(page), _fit(heads), _fit(hd), _act_t.index(k.dtype))
     c.tensors = (k, v)
     c.device = k.get_device()
     return c
@@ -406,8 +412,10 @@ def _check_cache(cache, dev):
 def wino_rope_frequencies(rotary_dim, theta, scaling=ROPE_SCALE_NONE, factor=1.0, orig_len=4096, turns_fast=32.0,
                           turns_slow=1.0):
     """(frequencies in radians per position, a list of rotary_dim/2 floats; the magnitude that goes with them)."""
-    out, mag = (C.c_double * max(rotary_dim // 2, 1))(), C.c_float()
-    c = wino_rope_config(rotary_dim, scaling, theta, factor, orig_len, turns_fast, turns_slow)
+    rotary_dim = _fit(rotary_dim)
+    # (no more than 65536 is accepted)
+    out, mag = (C.c_double * min(max(rotary_dim // 2, 1), 32768))(), C.c_float()
+    c = wino_rope_config(rotary_dim, _fit(scaling), theta, factor, orig_len, turns_fast, turns_slow)
     _check(lib.wino_rope_frequencies(C.byref(c), out, C.byref(mag)), "wino_rope_frequencies")
     return list(out), mag.value
 
@@ -436,7 +444,7 @@ def wino_rope_append(p: wino_rope_params, cache: wino_kv_cache, freq, pos, slot,
 
 
 def wino_attention_workspace_bytes(p: wino_attn_params, batch: int, total_q: int, max_kv_len: int) -> int:
-    return int(lib.wino_attention_workspace_bytes(p, batch, total_q, max_kv_len))
+    return int(lib.wino_attention_workspace_bytes(p, _fit(batch), _fit(total_q), _fit(max_kv_len)))
 
 
 def wino_paged_attention(p: wino_attn_params, cache: wino_kv_cache, q, out, cu_q, kv_len, page_table, max_kv_len,
@@ -453,8 +461,8 @@ def wino_paged_attention(p: wino_attn_params, cache: wino_kv_cache, q, out, cu_q
     width = page_table.shape[1]
     qs, os_ = _heads(q, a, h, hd, "q", dev, n), _heads(out, a, h, hd, "out", dev, n)
     _check(lib.wino_paged_attention(
-        p, cache, batch, n, max_kv_len, _op_ptr(cu_q, _i32_t, "cu_q", dev, batch + 1),
-        _op_ptr(kv_len, _i32_t, "kv_len", dev), table, width, width,
+        p, cache, _fit(batch), _fit(n), _fit(max_kv_len), _op_ptr(cu_q, _i32_t, "cu_q", dev, batch + 1),
+        _op_ptr(kv_len, _i32_t, "kv_len", dev), table, width, _fit(width),
         None if cur_start is None else _op_ptr(cur_start, _i32_t, "cur_start", dev, batch), qs, os_,
         None if lse is None else _op_ptr(lse, _f32_t, "lse", dev, n * h),
         None if workspace is None else _op_ptr(workspace, None, "workspace", dev),
@@ -471,7 +479,7 @@ def wino_packed_attention(p: wino_attn_params, q, k, v, out, cu_q, cu_k, max_kv_
     qs, os_ = _heads(q, a, h, hd, "q", dev, n), _heads(out, a, h, hd, "out", dev, n)
     ks, vs = _heads(k, a, hk, hd, "k", dev, nk), _heads(v, a, hk, hd, "v", dev, nk)
     _check(lib.wino_packed_attention(
-        p, batch, n, nk, max_kv_len, _op_ptr(cu_q, _i32_t, "cu_q", dev),
+        p, _fit(batch), _fit(n), _fit(nk), _fit(max_kv_len), _op_ptr(cu_q, _i32_t, "cu_q", dev),
         _op_ptr(cu_k, _i32_t, "cu_k", dev, batch + 1),
         None if cur_start is None else _op_ptr(cur_start, _i32_t, "cur_start", dev, batch), qs, ks, vs, os_,
         None if lse is None else _op_ptr(lse, _f32_t, "lse", dev, n * h),

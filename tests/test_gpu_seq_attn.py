@@ -516,3 +516,16 @@ def test_one_workspace_for_the_largest_sizes(P):
         ran_split += split(pr)
         assert (memory[need:] == 0xFF).all()
     assert ran_split >= 4
+
+
+def test_a_bound_of_the_lengths_beyond_32_bits_is_refused(P):
+    pr = Problem([(2, 100)], 4, 4, 64, 0)
+    pr.paged(P, 16)
+    args, ws = pr.last
+    for bound in ((1 << 32) + 50, 1 << 40, (1 << 63) + 100):
+        with pytest.raises(P.WinoError) as e:
+            P.wino_paged_attention(*args[:7], bound, workspace=ws)
+        assert e.value.status == -2
+        with pytest.raises(P.WinoError) as e:
+            P.wino_packed_attention(args[0], args[2], args[2], args[2], args[3], args[4], args[4], bound, workspace=ws)
+        assert e.value.status == -2

@@ -295,3 +295,22 @@ def test_documented_limits_of_rope(abi):
     with pytest.raises(abi.WinoError) as e:
         abi.wino_rope_frequencies(65538, 1e4)
     assert e.value.status == -2
+
+
+def test_integers_beyond_32_bits_are_refused(abi):
+    """The binding does not hand on the lower bits of a size that no 32-bit argument holds."""
+    p = abi.make_attn_params(8, 4, 64)
+    some = abi.wino_attention_workspace_bytes(p, 1, 1, 5000)
+    assert some > 0
+    for b, n, m in ((1, 1, (1 << 32) + 5000), (1, (1 << 32) + 1, 5000), ((1 << 32) + 1, 1, 5000), (1, 1, 5000 - (1 << 32))):
+        assert abi.wino_attention_workspace_bytes(p, b, n, m) == 0
+    for rotary_dim in ((1 << 32) + 64, 64 - (1 << 32), (1 << 40) + 64):
+        with pytest.raises(abi.WinoError) as e:
+            abi.wino_rope_frequencies(rotary_dim, 1e4)
+        assert e.value.status == -2
+    with pytest.raises(abi.WinoError):
+        abi.wino_rope_frequencies(64, 1e4, scaling=1 << 32)
+    assert abi.wino_attention_workspace_bytes(abi.make_attn_params((1 << 32) + 8, 4, 64), 1, 1, 5000) == 0
+    assert abi.wino_attention_workspace_bytes(abi.make_attn_params(8, 4, 64, mask=1 << 32), 1, 1, 5000) == 0
+    assert abi.make_rope_params(64, inverse=1 << 32).inverse == 1
+    assert abi.make_rope_params((1 << 32) + 64).head_dim == (1 << 31) - 1
