@@ -365,6 +365,22 @@ def _heads(x, act, n_heads, head_dim, name, dev, n_tokens) -> wino_heads:
     return wino_heads(x.data_ptr() or 16, ts if n_tokens > 1 else n_heads * head_dim, hs if n_heads > 1 else head_dim)
 
 
+def _table(x, batch, dev):
+    """Address, row stride and width of a page table: int32 [batch, width], the entries of a row side by side."""
+    if not isinstance(x, _Tensor):
+        raise TypeError("page_table: expected a torch tensor")
+    if x.get_device() != dev:
+        _wrong_device(x, dev, "page_table")
+    if x.dtype is not _i32_t:
+        raise TypeError(f"page_table: dtype {x.dtype}, expected {_i32_t}")
+    if x.dim() != 2 or x.shape[0] != batch:
+        raise ValueError(f"page_table: shape {tuple(x.shape)}, expected [{batch}, width]")
+    width = x.shape[1]
+    if width > 1 and x.stride(1) != 1:
+        raise ValueError("page_table: the last axis must be contiguous")
+    return x.data_ptr() or 16, x.stride(0) if batch > 1 else width, width
+
+
 def make_rope_params(head_dim, rotary_dim=None, layout=ROPE_HALF, dtype=ACT_BF16, magnitude=1.0,
                      inverse=False) -> wino_rope_params:
     return wino_rope_params(_fit(head_dim), _fit(head_dim if rotary_dim is None else rotary_dim), _fit(layout),
@@ -450,19 +466,17 @@ def wino_attention_workspace_bytes(p: wino_attn_params, batch: int, total_q: int
 def wino_paged_attention(p: wino_attn_params, cache: wino_kv_cache, q, out, cu_q, kv_len, page_table, max_kv_len,
                          cur_start=None, lse=None, workspace=None, stream=None) -> None:
     """Attention of the rows q [total_q, heads, head_dim] (sequence b: rows cu_q[b]..cu_q[b+1]) over the cache's pages
-    page_table int32 [batch, width], kv_len int32 [batch] keys each, at most max_kv_len.  lse: float32
-    [total_q, heads] or None; workspace: wino_attention_workspace_bytes, None if that is 0."""
+    page_table int32 [batch, width] (rows may be part of wider ones), kv_len int32 [batch] keys each, at most
+    max_kv_len.  lse: float32 [total_q, heads] or None; workspace: of wino_attention_workspace_bytes for these sizes or
+    larger ones, None if that is 0."""
     dev, a, h, hd = _current_device(), p.dtype, p.n_heads, p.head_dim
     _check_cache(cache, dev)
     n, batch = q.shape[0], kv_len.shape[0]
-    table = _op_ptr(page_table, _i32_t, "page_table", dev)
-    if page_table.dim() != 2 or page_table.shape[0] != batch:
-        raise ValueError(f"page_table: shape {tuple(page_table.shape)}, expected [{batch}, width]")
-    width = page_table.shape[1]
+    table, table_stride, width = _table(page_table, batch, dev)
     qs, os_ = _heads(q, a, h, hd, "q", dev, n), _heads(out, a, h, hd, "out", dev, n)
     _check(lib.wino_paged_attention(
         p, cache, _fit(batch), _fit(n), _fit(max_kv_len), _op_ptr(cu_q, _i32_t, "cu_q", dev, batch + 1),
-        _op_ptr(kv_len, _i32_t, "kv_len", dev), table, width, _fit(width),
+        _op_ptr(kv_len, _i32_t, "kv_len", dev), table, table_stride, _fit(width),
         None if cur_start is None else _op_ptr(cur_start, _i32_t, "cur_start", dev, batch), qs, os_,
         None if lse is None else _op_ptr(lse, _f32_t, "lse", dev, n * h),
         None if workspace is None else _op_ptr(workspace, None, "workspace", dev),

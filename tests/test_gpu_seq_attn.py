@@ -529,3 +529,30 @@ def test_a_bound_of_the_lengths_beyond_32_bits_is_refused(P):
         with pytest.raises(P.WinoError) as e:
             P.wino_packed_attention(args[0], args[2], args[2], args[2], args[3], args[4], args[4], bound, workspace=ws)
         assert e.value.status == -2
+
+
+def test_page_tables_inside_a_wider_one(P):
+    """The entries in use of a table with room for more, rows of a larger table, a table of one column."""
+    pr = Problem([(2, 100), (40, 61), (1, 9)], 4, 2, 64, 0, "causal")
+    want = pr.paged(P, 16)
+    args, ws = pr.last
+    table, out = args[6], torch.empty_like(args[3])
+    wide = torch.full((7, table.shape[1] + 9), -1, dtype=torch.int32, device="cuda")
+    for rows, first in ((slice(0, 3), 0), (slice(1, 7, 2), 5)):
+        wide.fill_(-1)
+        view = wide[rows, first:first + table.shape[1]]
+        view.copy_(table)
+        out.fill_(3)
+        P.wino_paged_attention(*args[:3], out, *args[4:6], view, args[7], workspace=ws)
+        assert torch.equal(out, want[0])
+    for view in (wide.t()[:3, :7], wide[:3, ::2], wide[:1, :7].expand(3, 7)[:, None, :]):
+        with pytest.raises(ValueError):
+            P.wino_paged_attention(*args[:3], out, *args[4:6], view, args[7], workspace=ws)
+    pr = Problem([(2, 16), (3, 5)], 4, 2, 64, 0, "causal")
+    want = pr.paged(P, 16)
+    args, ws = pr.last
+    P.wino_paged_attention(*args[:6], args[6].expand(-1, 1).t().contiguous().t(), args[7], workspace=ws)
+    wide[:2, 4:5] = args[6]
+    out = torch.empty_like(args[3])
+    P.wino_paged_attention(*args[:3], out, *args[4:6], wide[:2, 4:5], args[7], workspace=ws)
+    assert torch.equal(out, want[0]) and torch.equal(args[3], want[0])
