@@ -315,7 +315,7 @@ def _fit(n):
 
 def _current_device():
     try:
-        return _get_device()
+        return _get_device() if _get_device else _torch.cuda.current_device()
     except Exception:  # no device: there is no device tensor either
         return None
 

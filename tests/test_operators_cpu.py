@@ -314,3 +314,14 @@ def test_integers_beyond_32_bits_are_refused(abi):
     assert abi.wino_attention_workspace_bytes(abi.make_attn_params(8, 4, 64, mask=1 << 32), 1, 1, 5000) == 0
     assert abi.make_rope_params(64, inverse=1 << 32).inverse == 1
     assert abi.make_rope_params((1 << 32) + 64).head_dim == (1 << 31) - 1
+
+
+def test_current_device_without_the_private_call(abi, monkeypatch):
+    """torch's public call stands in where the private one does not exist."""
+    import torch
+    monkeypatch.setattr(abi, "_get_device", None)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 3)
+    assert abi._current_device() == 3
+    k = torch.zeros(1, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="must be a device tensor"):
+        abi._op_ptr(k, None, "k", abi._current_device())
