@@ -328,9 +328,9 @@ typedef struct {
  *                           keep f_j, those below turns_slow times take
  *                           f_j / factor, between them linear in the number
  *                           of turns; magnitude 0.1 ln(factor) + 1
- * WINO_ERR_INVALID_ARG: theta <= 1 or not finite, factor < 1 or not finite,
- * and for PARTS orig_len <= 0 or turns_fast <= turns_slow.  rotary_dim is even,
- * 2 to 65536 (WINO_ERR_SHAPE). */
+ * WINO_ERR_INVALID_ARG: theta <= 1 or not finite (scaled by BASE, too), factor
+ * < 1 or not finite, and for PARTS orig_len <= 0 or turns_fast <= turns_slow.
+ * rotary_dim is even, 2 to 65536 (WINO_ERR_SHAPE). */
 #define WINO_ROPE_SCALE_NONE 0
 #define WINO_ROPE_SCALE_LINEAR 1
 #define WINO_ROPE_SCALE_BASE 2

@@ -148,6 +148,7 @@ wino_status wino_rope_frequencies(const wino_rope_config* c, double* h_freq, flo
   const double r = c->rotary_dim, two_pi = 6.283185307179586476925286766559;
   double theta = c->theta;
   if (c->scaling == WINO_ROPE_SCALE_BASE) theta *= pow(c->factor, r / (r - 2));
+  if (!isfinite(theta)) return WINO_ERR_INVALID_ARG;
   for (int j = 0; j < c->rotary_dim / 2; ++j) {
     double f = pow(theta, -2.0 * j / r);
     if (c->scaling == WINO_ROPE_SCALE_LINEAR) f /= c->factor;

@@ -325,3 +325,11 @@ def test_current_device_without_the_private_call(abi, monkeypatch):
     k = torch.zeros(1, dtype=torch.bfloat16)
     with pytest.raises(ValueError, match="must be a device tensor"):
         abi._op_ptr(k, None, "k", abi._current_device())
+
+
+@pytest.mark.parametrize("rotary_dim,theta,factor", [(4, 1e4, 1e160), (64, 1e300, 1e10), (64, 1.7e308, 2.0)])
+def test_a_base_that_overflows_is_refused(abi, rotary_dim, theta, factor):
+    """theta times factor^(r/(r-2)) past the largest number: frequencies of zero are not the formula's."""
+    with pytest.raises(abi.WinoError) as e:
+        abi.wino_rope_frequencies(rotary_dim, theta, abi.ROPE_SCALE_BASE, factor)
+    assert e.value.status == -1
