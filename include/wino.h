@@ -274,9 +274,9 @@ wino_status wino_epilogue_noalloc(const wino_params* p, int32_t vocab, const voi
  * A tensor of rows: element e of head h of row t lies at
  * data[t * token_stride + h * head_stride + e].  Strides are in elements,
  * multiples of 8 and not negative; data is 16-byte aligned, and the token
- * strides of keys and values are below 2^26 (WINO_ERR_UNSUPPORTED otherwise).  Inputs may overlap or repeat (a stride of
- * 0); the rows and heads of an output must not (strides >= head_dim wherever
- * there is more than one). */
+ * strides of keys and values are below 2^26 (WINO_ERR_UNSUPPORTED otherwise).
+ * Inputs may overlap or repeat (a stride of 0); the rows and heads of an output
+ * must not (strides >= head_dim wherever there is more than one). */
 typedef struct {
   void* data;
   int64_t token_stride, head_stride;

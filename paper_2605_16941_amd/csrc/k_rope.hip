@@ -7,9 +7,10 @@
 // and past the rotated part 16 values that are copied.  A thread reads its
 // unit whole before it writes it, so a row may be rotated in place.
 //
-// A wave owns one token: its lanes first compute the token's cosines and
+// A wave works on one token, alone or, where tokens are few, beside others that
+// take shares of its head rows: its lanes first compute the token's cosines and
 // sines, one pair each, and share them through LDS; then hd/16 lanes per head
-// walk the token's head rows.  The angle is taken in 64 bits and reduced to a
+// walk the wave's head rows.  The angle is taken in 64 bits and reduced to a
 // fraction of a turn before the fp32 sine and cosine, so that position 2^20
 // is as exact as position 0.  Bound by memory: 4 bytes per value.
 #include "common.h"

@@ -12,16 +12,21 @@
 // join in LDS at the end.
 //
 // What bounds it, measured: few rows by memory (single tokens of 64 sequences
-// over 8192 keys each, 8 KV heads of 128: 374 us, 5.7 TB/s of keys and values),
+// over 8192 keys each, 8 KV heads of 128: 383 us, 5.6 TB/s of keys and values),
 // many rows by the matrix cores and the power they take (8192 x 8192, 32 heads of
-// 128: 1004 us, 1095 TFLOP/s), short sequences by the time until a workgroup's
-// first tile (64 rows over 544 keys of 16 sequences, 32 KV heads: 41 us).
+// 128: 977 us, 1125 TFLOP/s), short sequences by the time until a workgroup's
+// first tile (16 sequences of 64 rows, each over 544 keys, 32 KV heads: 41.5 us;
+// over 300 to 544 keys 35.8).
 //
 // Each wave computes S^T = K Q^T (32x32x16 MFMA), so a lane holds 16 keys per
 // 32-key block of ONE row and the softmax's running maximum and sum stay in
 // the lane (and its partner 32 apart); the same registers, rounded to the
 // type, are the B operand of O^T = V^T P^T.  One pass over the keys: O and the
-// sum are rescaled when the maximum moves.
+// sum are rescaled when the maximum moves.  The weights are rounded to the type
+// there (half a step of each; the sum takes them unrounded), as the products
+// with V have 16-bit operands: errors against 64 bits are 2.1-2.3e-3 (bf16) and
+// 2.1-2.9e-4 (fp16) in the 2-norm, of which the output's own rounding is 1.7e-3
+// and 2.0e-4.  Weights in two parts would double these products.
 //
 // K and V tiles go global -> LDS by LDS-DMA, double-buffered, 16-byte chunks
 // XOR-swizzled.  V lies in the cache as it was written, one token per row; its
@@ -181,7 +186,9 @@ __device__ __forceinline__ uint32_t nonfinite(uint32_t w) {
 // kernel), because the compiler otherwise waits for every copy in flight
 // before the next transposing read, which it takes for a write to LDS.  The
 // instruction's offset counts for both addresses; off[j] already has
-// 1024 (N - 1 - j) added and base 1024 (N - 1) subtracted.  s_nop 4: a scalar
+// 1024 (N - 1 - j) added and base 1024 (N - 1) subtracted.  m0 is a reserved
+// register: the compiler keeps nothing in it, and does not let it be named as
+// overwritten.  s_nop 4: a scalar
 // that the vector unit wrote (readfirstlane) may be read by a memory
 // instruction five wait states later, which the compiler does not see to here.
 template <int N>
@@ -761,7 +768,6 @@ __global__ __launch_bounds__(kThreads) void seq_attn_merge_kernel(AttnCall c, At
     const float l = valu_sum(ml.y < 0.f ? 0.f : w * ml.y);
     L += l;
     const int m = min(64, n - s0);
-#pragma unroll 4
     for (int s = 0; s < m; ++s) {
       const float ws = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), s));
       const float* q = p + (s0 + s) * rows * HD;
@@ -795,9 +801,13 @@ __global__ __launch_bounds__(kThreads) void seq_attn_merge_kernel(AttnCall c, At
 // that length and lengths spread evenly up to it.  Times measured on 28
 // problems (1-256 sequences, 1-2048 rows, 544-16000 keys, both head sizes) with
 // every chunk of 2^8..2^13 keys and none: the choice is 2% behind the best of
-// them in the mean and 8% at most; on 12 drawn ones 3% and 20%.  Measured both ways: one token of one
-// sequence over 8192 keys, 8 KV heads: 101 us whole, 24 us in chunks of 512;
-// 512 rows over 1000-4000 keys of 16 sequences: 249 us whole, 323 in 1024.
+// them in the mean and 8% at most; on 12 drawn ones 3% and 20%.  Measured both
+// ways: one token of one sequence over 8192 keys, 8 KV heads of 128: 127 us
+// whole, 24 in chunks of 256, which it takes (21 in 512); 4 sequences of 200-500
+// rows over 3000-16000 keys, 32 heads over 4 KV heads: 424 us whole, which it
+// takes, 482 in chunks of 1024 (397 in 4096: 7% that the times do not foresee).
+// slots: workgroups that run at once (64-wide heads over packed keys have 768 at
+// 128 rows; their times were fitted with 512).
 struct UnitTimes {
   int slots;
   float fix, full, alone;
