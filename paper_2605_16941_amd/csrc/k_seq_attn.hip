@@ -271,8 +271,10 @@ __global__ __launch_bounds__(attn_threads(QW), attn_waves(HD, QW, PAGED)) void s
   const int split = unit.rem / max(tiles, 1);
   const int row0 = (tiles - 1 - (unit.rem - split * tiles)) << RSHIFT;
   const int kbeg = split << pl.chunk_shift;
-  // (offsets that do not ascend count wrongly: nothing outside the tensors)
-  if (row0 < 0 || row0 >= n_rows || (split && kbeg >= sq.nkv)) return;
+  // Offsets that do not ascend count wrongly, past 32 bits where every sequence
+  // spans most rows: a unit is taken only if it is one of its sequence's, so that
+  // nothing outside the tensors is touched whatever the offsets.
+  if (row0 < 0 || row0 >= n_rows || split >= pl.splits || (split && kbeg >= sq.nkv)) return;
 
   const int tid = threadIdx.x, lane = tid & 63, grp = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);

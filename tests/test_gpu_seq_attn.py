@@ -556,3 +556,31 @@ def test_page_tables_inside_a_wider_one(P):
     out = torch.empty_like(args[3])
     P.wino_paged_attention(*args[:3], out, *args[4:6], wide[:2, 4:5], args[7], workspace=ws)
     assert torch.equal(out, want[0]) and torch.equal(args[3], want[0])
+
+
+@pytest.mark.parametrize("n,m", [(130, 200), (3, 1100), (130, 1100)])
+def test_offsets_in_any_order_stay_inside(P, n, m):
+    """Offsets that do not ascend and lengths of any sign: rows may be anything, but nothing around the outputs and the
+    workspace is written, and a later call is right."""
+    pr = Problem([(n, m), (1, 9), (7, m // 2)], 4, 2, 64, 0, "causal", seed=n)
+    want = pr.paged(P, 16)
+    args, _ = pr.last
+    total = args[2].shape[0]
+    need = P.wino_attention_workspace_bytes(args[0], 3, total, m)
+    memory = torch.full((need + 4096,), 0xFF, dtype=torch.uint8, device="cuda")
+    ws = memory[:need] if need else None
+    rng = np.random.default_rng(n)
+    for _ in range(6):
+        cu = pr.i32(rng.integers(-5, total + 50, 4).tolist())
+        lens = pr.i32(rng.integers(-5, m + 50, 3).tolist())
+        space = torch.full((total + 2, 4, 64), 3.0, dtype=torch.bfloat16, device="cuda")
+        lse = torch.full((total + 2, 4), 5.0, device="cuda")
+        P.wino_paged_attention(*args[:3], space[1:-1], cu, lens, *args[6:], lse=lse[1:-1], workspace=ws)
+        P.wino_packed_attention(args[0], args[2], args[2][:, :2], args[2][:, 2:], space[1:-1], cu, cu.flip(0), m,
+                                lse=lse[1:-1], workspace=ws)
+        torch.cuda.synchronize()
+        assert (space[0] == 3).all() and (space[-1] == 3).all() and (lse[0] == 5).all() and (lse[-1] == 5).all()
+        assert (memory[need:] == 0xFF).all()
+    out = torch.empty_like(args[3])
+    P.wino_paged_attention(*args[:3], out, *args[4:], workspace=ws)
+    assert torch.equal(out, want[0])
