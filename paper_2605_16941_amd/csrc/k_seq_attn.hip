@@ -917,6 +917,8 @@ hipError_t launch_hd(const AttnCall& c, hipStream_t st) {
 
 size_t attention_workspace(const AttnCall& c) { return (size_t)most_partial_rows(c) * (c.hd + 2) * 4; }
 
+bool attention_splits(const AttnCall& c) { return choose(c).splits > 1; }
+
 hipError_t launch_seq_attention(const AttnCall& c, hipStream_t st) {
   if (c.f16) return c.hd == 128 ? launch_hd<128, ActF16>(c, st) : launch_hd<64, ActF16>(c, st);
   return c.hd == 128 ? launch_hd<128, ActBf16>(c, st) : launch_hd<64, ActBf16>(c, st);

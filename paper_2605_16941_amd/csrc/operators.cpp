@@ -116,8 +116,8 @@ wino_status prepare_attn(const wino_attn_params* p, AttnCall& c, const int32_t* 
   wino_status s = check_heads(q, c.total_q, p->n_heads, p->head_dim, false);
   if (s == WINO_OK) s = check_heads(out, c.total_q, p->n_heads, p->head_dim, true);
   if (s != WINO_OK) return s;
-  const size_t need = attention_workspace(c);
-  if (need) {
+  if (attention_splits(c)) {
+    const size_t need = attention_workspace(c);
     if (!ws) return WINO_ERR_INVALID_ARG;
     if (ws_bytes < need) return WINO_ERR_SHAPE;
     if (reinterpret_cast<uintptr_t>(ws) % 16) return WINO_ERR_UNSUPPORTED;

@@ -53,7 +53,8 @@ struct AttnCall {
   int64_t page_stride;
   void* ws;
 };
-size_t attention_workspace(const AttnCall& c);
+size_t attention_workspace(const AttnCall& c);  // for these sizes and all smaller ones
+bool attention_splits(const AttnCall& c);       // whether this call uses it
 hipError_t launch_seq_attention(const AttnCall& c, hipStream_t st);
 
 }  // namespace wino

@@ -584,3 +584,15 @@ def test_offsets_in_any_order_stay_inside(P, n, m):
     out = torch.empty_like(args[3])
     P.wino_paged_attention(*args[:3], out, *args[4:], workspace=ws)
     assert torch.equal(out, want[0])
+
+
+@pytest.mark.parametrize("seqs", [[(300, 300), (70, 70)], [(600, 600)], [(1, 400), (1, 300)]])
+def test_calls_that_are_not_split_need_no_workspace(P, seqs):
+    """Where keys are not cut into chunks a call runs without memory, though smaller calls of the same program need some."""
+    pr = Problem(seqs, 4, 2, 64, 0, "causal")
+    assert P.wino_attention_workspace_bytes(pr.params(P), len(seqs), pr.cu(0)[-1], pr.seqs[0][1]) > 0
+    pr.check(pr.paged(P, 16))
+    assert not split(pr)
+    pr.workspace = lambda *a: None
+    pr.check(pr.paged(P, 16))
+    pr.check(pr.packed(P))
