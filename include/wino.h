@@ -399,9 +399,10 @@ typedef struct {
  * memory for a program's largest batch, total_q and max_kv_len serves its
  * smaller calls with the same heads, and at most 2^21 rows of head_dim + 2
  * floats.  A call that does not divide its keys runs without it; one that does
- * checks all of it.  Its contents mean nothing between calls; calls that may overlap need
- * one each.  max_kv_len bounds every sequence's n_kv: longer ones are cut to
- * it.  The nearer it is to the longest, the better the work is divided. */
+ * checks all of it.  Its contents mean nothing between calls; calls that may
+ * overlap need one each.  max_kv_len bounds every sequence's n_kv: longer ones
+ * are cut to it.  The nearer it is to the longest, the better the work is
+ * divided. */
 size_t wino_attention_workspace_bytes(const wino_attn_params* p, int32_t batch, int32_t total_q,
                                       int32_t max_kv_len);
 
